@@ -271,6 +271,84 @@ int flexiq_mixed_conv_to_slab(flexiq_layer_t layer, const uint8_t *X4_dev, const
                               flexiq_layer_t next_layer, float next_x_scale, int relu,
                               int out_order, uint8_t *next_X4_dev, void *stream);
 
+/* ---- Operators between the quantized layers ----
+ *
+ * The evaluation keeps normalisation, activation functions and residual additions in floating point between
+ * the quantized layers.  These calls do them where the data already is: in a layer's epilogue, and in one pass
+ * from a floating-point tensor to a normalised one or to the next layer's slab.
+ *
+ * act: the activation function.  Evaluated in fp32; infinities give the functions' limits, NaNs stay NaN. */
+#define FLEXIQ_ACT_NONE 0
+#define FLEXIQ_ACT_RELU 1      /* max(v, 0)                                                    */
+#define FLEXIQ_ACT_GELU 2      /* v Phi(v), Phi the normal distribution function               */
+#define FLEXIQ_ACT_GELU_TANH 3 /* v (1 + tanh(sqrt(2/pi) (v + 0.044715 v^3))) / 2              */
+#define FLEXIQ_ACT_SILU 4      /* v / (1 + exp(-v))                                            */
+/* residual_order: where the residual enters */
+#define FLEXIQ_RESIDUAL_AFTER_ACT 0  /* y = act(v) + r: a transformer's residual stream */
+#define FLEXIQ_RESIDUAL_BEFORE_ACT 1 /* y = act(v + r): the end of a ResNet block       */
+
+/* flexiq_mixed_gemm / flexiq_mixed_conv with an activation and a residual in the epilogue.  With
+ *   v = fma(float(acc), x_scale*w_scale[n], bias[n])            (the DEQUANT_F32 value)
+ *   y = act(v) + r  or  act(v + r)                              (fp32, each addition rounded once)
+ * the output is
+ *   DEQUANT_F32: y;  DEQUANT_F16 / DEQUANT_BF16: y rounded to nearest even
+ *   REQUANT_I8 : clip(round_half_even(y / y_scale), -128, 127)  (what flexiq_quantize_lower makes of y, before lowering)
+ * With FLEXIQ_ACT_NONE and no residual the floating-point outputs equal flexiq_mixed_gemm's bit for bit.
+ *   residual_dev   row-major in the output's shape ([M][N], or [Nb][P][Q][Cout]), 16-byte aligned, or NULL for
+ *                  none; residual_dtype F32, F16 or BF16, whatever the output's type
+ *   Y_dev          may be residual_dev itself when both have the same type (the residual stream updated in
+ *                  place); any other overlap of the two is not allowed.  FLEXIQ_OUT_ACC_I32 is refused.
+ * Otherwise as flexiq_mixed_gemm / flexiq_mixed_conv. */
+int flexiq_mixed_gemm_act(flexiq_layer_t layer, const uint8_t *X4_dev, const int8_t *X8_dev,
+                          const uint8_t *x_shift_dev, int64_t M, float x_scale, float y_scale, int act,
+                          const void *residual_dev, int residual_dtype, int residual_order, int out_mode,
+                          void *Y_dev, void *stream);
+int flexiq_mixed_conv_act(flexiq_layer_t layer, const uint8_t *X4_dev, const int8_t *X8_dev,
+                          const uint8_t *x_shift_dev, int Nb, int H, int W, float x_scale, float y_scale, int act,
+                          const void *residual_dev, int residual_dtype, int residual_order, int out_mode,
+                          void *Y_dev, void *stream);
+
+/* The fused layer boundary with an activation function between the two layers: per output element what
+ *   flexiq_mixed_gemm_act(..., act, no residual, DEQUANT_F32)
+ *   flexiq_quantize_lower(next_layer, ., FLEXIQ_DTYPE_F32, next_x_scale, static positions)
+ * compute, bit for bit.  (flexiq_mixed_gemm_to_slab folds the next scale into the factors instead, and
+ * so rounds differently.)  Otherwise as flexiq_mixed_gemm_to_slab / flexiq_mixed_conv_to_slab. */
+int flexiq_mixed_gemm_act_to_slab(flexiq_layer_t layer, const uint8_t *X4_dev, const int8_t *X8_dev,
+                                  const uint8_t *x_shift_dev, int64_t M, float x_scale,
+                                  flexiq_layer_t next_layer, float next_x_scale, int act, int out_order,
+                                  uint8_t *next_X4_dev, void *stream);
+int flexiq_mixed_conv_act_to_slab(flexiq_layer_t layer, const uint8_t *X4_dev, const int8_t *X8_dev,
+                                  const uint8_t *x_shift_dev, int Nb, int H, int W, float x_scale,
+                                  flexiq_layer_t next_layer, float next_x_scale, int act, int out_order,
+                                  uint8_t *next_X4_dev, void *stream);
+
+/* Group normalisation of a channels-last tensor, followed by an activation:
+ *   y[i][p][c] = act((x[i][p][c] - mean) / sqrt(var + eps) * gamma[c] + beta[c])
+ * mean and (biased) var over the P positions of image i and the C / groups channels of c's group.  One group and
+ * P = 1 is layer normalisation of Nb rows.  Statistics, and everything up to the output's rounding, in fp32.
+ *   X_dev    [Nb][P][C], x_dtype F32, F16 or BF16
+ *   gamma_dev, beta_dev  [C] fp32, or NULL (1 and 0)
+ *   eps      positive
+ *   Y_dev    [Nb][P][C], y_dtype F32, F16 or BF16; may be X_dev itself when the types are the same
+ *   scratch_dev  device memory of the size flexiq_group_norm_scratch gives (16-byte aligned; NULL where that is
+ *            0), written and read by this call's kernels: calls whose kernels may overlap need one each
+ * C is any multiple of groups.  X_dev, Y_dev, gamma_dev and beta_dev 16-byte aligned.  Nb == 0 or P == 0 is a
+ * successful no-op.  Enqueued on `stream` of the current device; nothing is allocated. */
+int flexiq_group_norm(const void *X_dev, int x_dtype, int64_t Nb, int64_t P, int C, int groups,
+                      const float *gamma_dev, const float *beta_dev, float eps, int act, int y_dtype, void *Y_dev,
+                      void *scratch_dev, void *stream);
+/* Bytes of scratch flexiq_group_norm and flexiq_group_norm_to_slab need for a shape (host-only). */
+int flexiq_group_norm_scratch(int x_dtype, int64_t Nb, int64_t P, int C, int groups, int64_t *bytes_out);
+
+/* The same, into the activation slab of `layer` (C = its input channels) in place of a floating-point tensor:
+ * what flexiq_group_norm(..., y_dtype F32) and flexiq_quantize_lower(layer, ., FLEXIQ_DTYPE_F32, Nb * P, x_scale,
+ * static positions) compute, bit for bit, in one pass over X_dev.
+ *   layer    on the MASKED path; its ratio at the time of this call decides the lowering
+ *   X4_dev   [Nb * P][C] the layer's slab, 16-byte aligned */
+int flexiq_group_norm_to_slab(flexiq_layer_t layer, const void *X_dev, int x_dtype, int64_t Nb, int64_t P, int groups,
+                              const float *gamma_dev, const float *beta_dev, float eps, int act, float x_scale,
+                              uint8_t *X4_dev, void *scratch_dev, void *stream);
+
 /* ---- Calibration on the device (off the hot path; produces what flexiq_layer_create_* takes) ----
  *
  * flexiq_calib_channel_ranges: per input channel the range [lo, hi] (lo <= 0 <= hi) of the

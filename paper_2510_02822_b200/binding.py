@@ -19,6 +19,8 @@ OUT_ACC_I32, OUT_REQUANT_I8, OUT_DEQUANT_F32 = 0, 1, 2
 OUT_DEQUANT_F16, OUT_DEQUANT_BF16 = 4, 5
 LOWBIT_MASKED_I8, LOWBIT_PACKED_U4 = 0, 1
 ORDER_ORIGINAL, ORDER_NEXT_SLAB = 0, 1
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2, 3, 4
+RESIDUAL_AFTER_ACT, RESIDUAL_BEFORE_ACT = 0, 1
 REORDER_TO_SLAB, REORDER_FROM_SLAB = 0, 1
 
 EXPORTS = [
@@ -26,6 +28,8 @@ EXPORTS = [
     "flexiq_layer_set_group_perm", "flexiq_layers_set_group_perm", "flexiq_layer_set_lowbit_path", "flexiq_layer_sync_ratio", "flexiq_layer_set_slab_check", "flexiq_set_lowbit_ratio", "flexiq_get_max_4bit_ch",
     "flexiq_x4_pitch", "flexiq_quantize_lower", "flexiq_quantize_lower_dynamic_noalloc", "flexiq_mixed_gemm", "flexiq_mixed_conv",
     "flexiq_mixed_gemm_to_slab", "flexiq_mixed_conv_to_slab", "flexiq_reorder_channels",
+    "flexiq_mixed_gemm_act", "flexiq_mixed_conv_act", "flexiq_mixed_gemm_act_to_slab", "flexiq_mixed_conv_act_to_slab",
+    "flexiq_group_norm", "flexiq_group_norm_scratch", "flexiq_group_norm_to_slab",
     "flexiq_calib_channel_ranges", "flexiq_calib_channel_histogram", "flexiq_calib_ranges_from_histogram",
     "flexiq_calib_weight_absmax", "flexiq_calib_prepare", "flexiq_calib_static", "flexiq_calib_absmax_ema",
     "flexiq_controller_create", "flexiq_controller_destroy", "flexiq_controller_level", "flexiq_controller_update",
@@ -70,6 +74,13 @@ def lib():
         L.flexiq_mixed_conv.argtypes = [vp, vp, vp, vp, i32, i32, i32, f32, f32, i32, vp, vp]
         L.flexiq_mixed_gemm_to_slab.argtypes = [vp, vp, vp, vp, i64, f32, vp, f32, i32, i32, vp, vp]
         L.flexiq_mixed_conv_to_slab.argtypes = [vp, vp, vp, vp, i32, i32, i32, f32, vp, f32, i32, i32, vp, vp]
+        L.flexiq_mixed_gemm_act.argtypes = [vp, vp, vp, vp, i64, f32, f32, i32, vp, i32, i32, i32, vp, vp]
+        L.flexiq_mixed_conv_act.argtypes = [vp, vp, vp, vp, i32, i32, i32, f32, f32, i32, vp, i32, i32, i32, vp, vp]
+        L.flexiq_mixed_gemm_act_to_slab.argtypes = [vp, vp, vp, vp, i64, f32, vp, f32, i32, i32, vp, vp]
+        L.flexiq_mixed_conv_act_to_slab.argtypes = [vp, vp, vp, vp, i32, i32, i32, f32, vp, f32, i32, i32, vp, vp]
+        L.flexiq_group_norm.argtypes = [vp, i32, i64, i64, i32, i32, vp, vp, f32, i32, i32, vp, vp, vp]
+        L.flexiq_group_norm_scratch.argtypes = [i32, i64, i64, i32, i32, C.POINTER(i64)]
+        L.flexiq_group_norm_to_slab.argtypes = [vp, vp, i32, i64, i64, i32, vp, vp, f32, i32, f32, vp, vp, vp]
         L.flexiq_reorder_channels.argtypes = [vp, vp, i32, i64, i32, vp, vp]
         L.flexiq_calib_channel_ranges.argtypes = [vp, i32, i64, i32, f32, i32, vp, vp, vp]
         L.flexiq_calib_channel_histogram.argtypes = [vp, i32, i64, i32, f32, i32, vp, vp]
@@ -235,6 +246,42 @@ def flexiq_mixed_conv_to_slab(h, X4_dev, X8_dev, x_shift_dev, Nb, H, W, x_scale,
                                            next_x_scale, int(relu), out_order, _ptr(next_X4_dev), _stream()))
 
 
+def flexiq_mixed_gemm_act(h, X4_dev, X8_dev, x_shift_dev, M, x_scale, y_scale, act, residual_dev, residual_dtype, residual_order, out_mode, Y_dev):
+    _check(lib().flexiq_mixed_gemm_act(h, _ptr(X4_dev), _ptr(X8_dev), _ptr(x_shift_dev), M, x_scale, y_scale, act, _ptr(residual_dev),
+                                       residual_dtype, residual_order, out_mode, _ptr(Y_dev), _stream()))
+
+
+def flexiq_mixed_conv_act(h, X4_dev, X8_dev, x_shift_dev, Nb, H, W, x_scale, y_scale, act, residual_dev, residual_dtype, residual_order, out_mode, Y_dev):
+    _check(lib().flexiq_mixed_conv_act(h, _ptr(X4_dev), _ptr(X8_dev), _ptr(x_shift_dev), Nb, H, W, x_scale, y_scale, act, _ptr(residual_dev),
+                                       residual_dtype, residual_order, out_mode, _ptr(Y_dev), _stream()))
+
+
+def flexiq_mixed_gemm_act_to_slab(h, X4_dev, X8_dev, x_shift_dev, M, x_scale, next_h, next_x_scale, act, out_order, next_X4_dev):
+    _check(lib().flexiq_mixed_gemm_act_to_slab(h, _ptr(X4_dev), _ptr(X8_dev), _ptr(x_shift_dev), M, x_scale, next_h, next_x_scale, act,
+                                               out_order, _ptr(next_X4_dev), _stream()))
+
+
+def flexiq_mixed_conv_act_to_slab(h, X4_dev, X8_dev, x_shift_dev, Nb, H, W, x_scale, next_h, next_x_scale, act, out_order, next_X4_dev):
+    _check(lib().flexiq_mixed_conv_act_to_slab(h, _ptr(X4_dev), _ptr(X8_dev), _ptr(x_shift_dev), Nb, H, W, x_scale, next_h, next_x_scale, act,
+                                               out_order, _ptr(next_X4_dev), _stream()))
+
+
+def flexiq_group_norm(X_dev, x_dtype, Nb, P, C_, groups, gamma_dev, beta_dev, eps, act, y_dtype, Y_dev, scratch_dev=None):
+    _check(lib().flexiq_group_norm(_ptr(X_dev), x_dtype, Nb, P, C_, groups, _ptr(gamma_dev), _ptr(beta_dev), eps, act, y_dtype, _ptr(Y_dev),
+                                   _ptr(scratch_dev), _stream()))
+
+
+def flexiq_group_norm_scratch(x_dtype, Nb, P, C_, groups) -> int:
+    v = C.c_int64()
+    _check(lib().flexiq_group_norm_scratch(x_dtype, Nb, P, C_, groups, C.byref(v)))
+    return v.value
+
+
+def flexiq_group_norm_to_slab(h, X_dev, x_dtype, Nb, P, groups, gamma_dev, beta_dev, eps, act, x_scale, X4_dev, scratch_dev=None):
+    _check(lib().flexiq_group_norm_to_slab(h, _ptr(X_dev), x_dtype, Nb, P, groups, _ptr(gamma_dev), _ptr(beta_dev), eps, act, x_scale,
+                                           _ptr(X4_dev), _ptr(scratch_dev), _stream()))
+
+
 def flexiq_reorder_channels(h, X_dev, elem_bytes, M, direction, Y_dev):
     _check(lib().flexiq_reorder_channels(h, _ptr(X_dev), elem_bytes, M, direction, _ptr(Y_dev), _stream()))
 
@@ -317,6 +364,71 @@ def _dtype_code(t):
         _TORCH_DTYPE.update({torch.float32: DTYPE_F32, torch.float16: DTYPE_F16, torch.bfloat16: DTYPE_BF16,
                              torch.int8: DTYPE_I8})
     return _TORCH_DTYPE[t.dtype]
+
+
+def _refuse(ok, message):
+    if not ok:
+        raise FlexiqError(ERR_INVALID_ARG, message)
+
+
+def _check_tensor(t, what, numel, device, dtypes):
+    """What the library takes as it is: a contiguous tensor on `device`, of this many elements and one of these types."""
+    _refuse(t.is_cuda and t.device == device and t.is_contiguous() and t.numel() == numel and t.dtype in dtypes,
+            f"{what} must be a contiguous tensor of {numel} elements on {device}, of type {' or '.join(str(d) for d in dtypes)}")
+
+
+def _float_types():
+    import torch
+    return torch.float32, torch.float16, torch.bfloat16
+
+
+def _out_dtype(out_mode):
+    import torch
+    dt = {OUT_REQUANT_I8: torch.int8, OUT_DEQUANT_F32: torch.float32, OUT_DEQUANT_F16: torch.float16, OUT_DEQUANT_BF16: torch.bfloat16}.get(out_mode)
+    _refuse(dt is not None, f"out_mode {out_mode} is not one of the outputs after an activation or a residual")
+    return dt
+
+
+def _norm_args(X, gamma, beta):
+    """(images, positions, channels) of a channels-last tensor [images, ..., channels]; refuses what the library does not take."""
+    import math
+    import torch
+    _refuse(X.dim() >= 2 and X.is_cuda and X.is_contiguous() and X.dtype in _float_types(),
+            "X must be a contiguous channels-last tensor [images, ..., channels] on a CUDA device, of type float32, float16 or bfloat16")
+    _refuse(X.device.index == torch.cuda.current_device(), f"X lies on {X.device}, which is not the current device")
+    for t, what in ((gamma, "gamma"), (beta, "beta")):
+        if t is not None:
+            _check_tensor(t, what, X.shape[-1], X.device, (torch.float32,))
+    return X.shape[0], math.prod(X.shape[1:-1]), X.shape[-1]
+
+
+def _norm_scratch(X, Nb, P, C_, groups):
+    import torch
+    n = flexiq_group_norm_scratch(_dtype_code(X), Nb, P, C_, groups)
+    return torch.empty(n, dtype=torch.uint8, device=X.device) if n else None
+
+
+def group_norm(X, groups, gamma=None, beta=None, eps=1e-5, act=ACT_NONE, out_dtype=None, Y=None):
+    """act((X - mean) / sqrt(var + eps) * gamma + beta) of a channels-last tensor [images, ..., channels], mean and variance per image and
+    group of channels (flexiq_group_norm).  groups = 1 on a [rows, channels] tensor is layer normalisation.  out_dtype: X's by default."""
+    import torch
+    native = _native_calls()
+    codes = {torch.float32: DTYPE_F32, torch.float16: DTYPE_F16, torch.bfloat16: DTYPE_BF16}
+    if out_dtype is None:
+        out_dtype = X.dtype if Y is None else Y.dtype
+    code = codes.get(out_dtype)
+    _refuse(code is not None, f"out_dtype {out_dtype} is not float32, float16 or bfloat16")
+    if native is not None:
+        r = native.group_norm(X, groups, gamma, beta, eps, act, code, Y)
+        if r is not NotImplemented:
+            return r
+    Nb, P, channels = _norm_args(X, gamma, beta)
+    if Y is None:
+        Y = torch.empty(X.shape, dtype=out_dtype, device=X.device)
+    else:
+        _check_tensor(Y, "Y", X.numel(), X.device, (out_dtype,))
+    flexiq_group_norm(X, _dtype_code(X), Nb, P, channels, groups, gamma, beta, eps, act, code, Y, _norm_scratch(X, Nb, P, channels, groups))
+    return Y
 
 
 class Layer:
@@ -456,6 +568,90 @@ class Layer:
         if slab is None:
             slab = nxt.alloc_slabs(Nb * P * Q)[0]
         flexiq_mixed_conv_to_slab(self.h, x4, x8, x_shift, Nb, H, W, x_scale, nxt.h, next_x_scale, relu, out_order, slab)
+        return slab
+
+    def _out_pixels(self, H, W):
+        stride, pad = self.conv
+        _refuse(H + 2 * pad >= self.R and W + 2 * pad >= self.S, "filter does not fit the padded input")
+        return (H + 2 * pad - self.R) // stride + 1, (W + 2 * pad - self.S) // stride + 1
+
+    def _act_args(self, shape, out_mode, residual, Y):
+        """The output tensor and the residual's type code; refuses tensors that do not fit."""
+        import math
+        import torch
+        dt, n = _out_dtype(out_mode), math.prod(shape)
+        if residual is not None:
+            _check_tensor(residual, "residual", n, self.device, _float_types())
+        if Y is None:
+            Y = torch.empty(shape, dtype=dt, device=self.device)
+        else:
+            _check_tensor(Y, "Y", n, self.device, (dt,))
+        return Y, 0 if residual is None else _dtype_code(residual)
+
+    def _act_slab(self, slab, rows):
+        if slab is None:
+            return self.alloc_slabs(rows)[0]
+        _refuse(slab.is_cuda and slab.device == self.device and slab.is_contiguous() and slab.element_size() == 1 and slab.numel() >= rows * self.K,
+                f"slab must be a contiguous one-byte tensor of at least {rows * self.K} elements on {self.device}")
+        return slab
+
+    def mixed_gemm_act(self, x4, x8, M, x_scale, act, out_mode, residual=None, residual_order=RESIDUAL_AFTER_ACT, y_scale=1.0, Y=None, x_shift=None):
+        """mixed_gemm with an activation and a residual [M, N] in its epilogue: act(v) + residual, or act(v + residual)
+        (flexiq_mixed_gemm_act).  Y may be the residual itself."""
+        if self._calls is not None:
+            r = self._calls.mixed_gemm_act(x4, x8, M, x_scale, x_shift, act, out_mode, residual, residual_order, y_scale, Y)
+            if r is not NotImplemented:
+                return r
+        _refuse(M >= 0, f"M = {M} is negative")
+        Y, code = self._act_args((M, self.N), out_mode, residual, Y)
+        flexiq_mixed_gemm_act(self.h, x4, x8, x_shift, M, x_scale, y_scale, act, residual, code, residual_order, out_mode, Y)
+        return Y
+
+    def mixed_conv_act(self, x4, x8, Nb, H, W, x_scale, act, out_mode, residual=None, residual_order=RESIDUAL_AFTER_ACT, y_scale=1.0, Y=None, x_shift=None):
+        """mixed_conv with an activation and a residual in the output's shape (flexiq_mixed_conv_act)."""
+        if self._calls is not None:
+            r = self._calls.mixed_conv_act(x4, x8, Nb, H, W, x_scale, x_shift, act, out_mode, residual, residual_order, y_scale, Y)
+            if r is not NotImplemented:
+                return r
+        _refuse(self.conv is not None and Nb >= 0, "mixed_conv_act needs a convolution layer and a number of images")
+        Y, code = self._act_args((Nb, *self._out_pixels(H, W), self.N), out_mode, residual, Y)
+        flexiq_mixed_conv_act(self.h, x4, x8, x_shift, Nb, H, W, x_scale, y_scale, act, residual, code, residual_order, out_mode, Y)
+        return Y
+
+    def mixed_gemm_act_to_slab(self, x4, x8, M, x_scale, nxt, next_x_scale, act, slab=None, x_shift=None, out_order=ORDER_ORIGINAL):
+        """Fused layer boundary with an activation: mixed_gemm_act to fp32, then nxt.quantize_lower, in one launch."""
+        nxt_calls = getattr(nxt, "_calls", None)
+        if self._calls is not None and nxt_calls is not None:
+            r = self._calls.mixed_gemm_act_to_slab(x4, x8, M, x_scale, nxt_calls, next_x_scale, act, slab, x_shift, out_order)
+            if r is not NotImplemented:
+                return r
+        _refuse(M >= 0, f"M = {M} is negative")
+        slab = nxt._act_slab(slab, M)
+        flexiq_mixed_gemm_act_to_slab(self.h, x4, x8, x_shift, M, x_scale, nxt.h, next_x_scale, act, out_order, slab)
+        return slab
+
+    def mixed_conv_act_to_slab(self, x4, x8, Nb, H, W, x_scale, nxt, next_x_scale, act, slab=None, x_shift=None, out_order=ORDER_ORIGINAL):
+        nxt_calls = getattr(nxt, "_calls", None)
+        if self._calls is not None and nxt_calls is not None:
+            r = self._calls.mixed_conv_act_to_slab(x4, x8, Nb, H, W, x_scale, nxt_calls, next_x_scale, act, slab, x_shift, out_order)
+            if r is not NotImplemented:
+                return r
+        _refuse(self.conv is not None and Nb >= 0, "mixed_conv_act_to_slab needs a convolution layer and a number of images")
+        P, Q = self._out_pixels(H, W)
+        slab = nxt._act_slab(slab, Nb * P * Q)
+        flexiq_mixed_conv_act_to_slab(self.h, x4, x8, x_shift, Nb, H, W, x_scale, nxt.h, next_x_scale, act, out_order, slab)
+        return slab
+
+    def group_norm_to_slab(self, X, groups, gamma, beta, x_scale, eps=1e-5, act=ACT_NONE, slab=None):
+        """group_norm to fp32, then quantize_lower, in one pass: writes this layer's slab and returns it (flexiq_group_norm_to_slab)."""
+        if self._calls is not None:
+            r = self._calls.group_norm_to_slab(X, groups, gamma, beta, eps, act, x_scale, slab)
+            if r is not NotImplemented:
+                return r
+        Nb, P, channels = _norm_args(X, gamma, beta)
+        _refuse(channels == self.K and X.device == self.device, f"X has {channels} channels on {X.device}, the layer takes {self.K} on {self.device}")
+        slab = self._act_slab(slab, Nb * P)
+        flexiq_group_norm_to_slab(self.h, X, _dtype_code(X), Nb, P, groups, gamma, beta, eps, act, x_scale, slab, _norm_scratch(X, Nb, P, channels, groups))
         return slab
 
     def mixed_conv(self, x4, x8, Nb, H, W, x_scale, y_scale, out_mode, Y=None, x_shift=None):

@@ -14,7 +14,7 @@ CSRC = os.path.join(_DIR, "csrc")
 LIB = os.path.join(_DIR, "libflexiq.so")
 CALLS = os.path.join(_DIR, "_calls.so")
 CALLS_FOR = os.path.join(_DIR, "_calls.stamp")   # the Python and torch that _calls.so was built for
-SOURCES = ["flexiq_layer.cu", "flexiq_prologue.cu", "flexiq_gemm.cu", "flexiq_reorder.cu", "flexiq_calib.cu", "flexiq_serving.cu", "flexiq_evolution.cu"]
+SOURCES = ["flexiq_layer.cu", "flexiq_prologue.cu", "flexiq_gemm.cu", "flexiq_reorder.cu", "flexiq_norm.cu", "flexiq_calib.cu", "flexiq_serving.cu", "flexiq_evolution.cu"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "--fmad=false",  # the epilogue spells out its fused multiply-adds; nothing else may contract

@@ -115,6 +115,10 @@ inline QuotientPlan plan_quotient(float S, int dtype)
     return p;
 }
 
+// The plan for a layer's scale, kept with the layer (flexiq_prologue.cu).
+struct Layer;
+QuotientPlan quotient_plan(Layer *L, float S, int dtype);
+
 // two int32 -> two saturated int8 in the low half, upper half taken from c's low half
 __device__ __forceinline__ unsigned pack2_sat_s8(int hi, int lo, unsigned c)
 {

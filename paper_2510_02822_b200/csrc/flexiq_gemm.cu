@@ -25,6 +25,8 @@
 #include "sm100_ptx.cuh"
 #include "copy_ring.cuh"
 #include "straddle.cuh"
+#include "eq1_quantize.cuh"
+#include "activation.cuh"
 #include "role_timers.cuh"   // PROF_* expand to nothing in the product build
 
 namespace flexiq {
@@ -52,7 +54,9 @@ constexpr int kOutScatter = 6;
 // A kernel serves one kind of output.  One kernel for all of them spilled registers in every epilogue (ptxas, per thread: 160 bytes stored
 // and 180 loaded in the plain CTA pair, 108 and 244 in the single CTA, none in either now), and the epilogue is as long as the mainloop
 // at short K.  Packed path, 768 -> 3072 at 12,608 rows 60.7 -> 57.1 us, 384 -> 1536 at 1576 8.9 -> 7.8.
-enum OutKind { kKindI8, kKindNext, kKindScatter, kKindHalf, kKindWord };
+// The kinds from kKindActI8 on apply an activation and add a residual: more instructions and registers, and so kernels of their own.
+enum OutKind { kKindI8, kKindNext, kKindScatter, kKindHalf, kKindWord, kKindActI8, kKindActNext, kKindActScatter, kKindActHalf, kKindActWord };
+constexpr int kActKinds = kKindActI8 - kKindI8;
 static OutKind out_kind(int out_mode, bool staged)
 {
     return out_mode == FLEXIQ_OUT_REQUANT_I8 ? kKindI8 : out_mode == kOutNextSlab ? (staged ? kKindNext : kKindScatter)
@@ -86,6 +90,12 @@ struct GemmParams {
     const int32_t *next_ent;   // [N/16] slab position (in chunks) of original chunk c | its group's position << 24
     int next_K_lo;             // the next layer's max_4bit_ch
     int relu;                  // clamp at zero before the re-quantization
+    // activation and residual (the kinds from kKindActI8 on)
+    int act;                   // FLEXIQ_ACT_*
+    const void *res;           // [M][N] in Y's order, or NULL
+    int res_dtype, res_first;  // FLEXIQ_DTYPE_*; added before the activation
+    QuotientPlan quot;         // int8 outputs: the division by q_scale
+    float q_scale;
     // Resident weights (convolutions on the multi-tap path whose output channels fit one tile): every tap's
     // weight tile is loaded once per CTA and stays in shared memory in front of the ring, whose stages then hold
     // activation taps only: half as many copies per tile for the producer lane, which bounds these layers.
@@ -203,13 +213,6 @@ struct PixelWalk {
     }
 };
 
-// two int32 -> two saturated int8 in the low half, upper half taken from c's low half
-__device__ __forceinline__ unsigned pack2_sat_s8(int hi, int lo, unsigned c)
-{
-    unsigned d;
-    asm("cvt.pack.sat.s8.s32.b32 %0, %1, %2, %3;" : "=r"(d) : "r"(hi), "r"(lo), "r"(c));
-    return d;
-}
 // round-half-even, saturate to int8, pack little-endian (y0 in the lowest byte)
 __device__ __forceinline__ unsigned requant4(float y0, float y1, float y2, float y3)
 {
@@ -289,6 +292,53 @@ __device__ __forceinline__ void next_slab16(const GemmParams &p, int ent, const 
         for (int q = 0; q < 4; ++q) out[q] &= mask;
     }
 }
+// Activation and residual: 16 accumulator columns of one row -> 16 fp32 values.  `res` = the row's residual at these columns, or NULL.
+__device__ __forceinline__ void add_residual16(int dtype, const void *res, float *v)
+{
+    float x[16];
+    if (dtype == FLEXIQ_DTYPE_F32) load16<FLEXIQ_DTYPE_F32>(res, x);
+    else if (dtype == FLEXIQ_DTYPE_F16) load16<FLEXIQ_DTYPE_F16>(res, x);
+    else load16<FLEXIQ_DTYPE_BF16>(res, x);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = __fadd_rn(v[i], x[i]);
+}
+__device__ __forceinline__ void finish16_act(const GemmParams &p, const uint32_t *r, const float *alpha16, const float *beta16, const void *res, float *v)
+{
+    finish16<FLEXIQ_OUT_DEQUANT_F32>(r, alpha16, beta16, reinterpret_cast<uint32_t *>(v));
+    if (res && p.res_first) add_residual16(p.res_dtype, res, v);
+    activate_n<16>(p.act, v);
+    if (res && !p.res_first) add_residual16(p.res_dtype, res, v);
+}
+// Eq. 1 of 16 values, clipped to the integers lo and hi first: what the prologue makes of them
+__device__ __forceinline__ void quantize16_f32(const GemmParams &p, const float *v, float lo, float hi, uint32_t mask, uint32_t *out)
+{
+    float t[16];
+    if (p.quot.form == kQuotTwoTerm) {
+        const TwoTerm div{p.quot.r_hi, p.quot.r_lo};
+#pragma unroll
+        for (int i = 0; i < 16; ++i) t[i] = TwoTerm::clip(div(v[i]), lo, hi);
+    } else {
+        const Divider div = make_divider(p.q_scale);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) t[i] = Divider::clip(div(v[i]), lo, hi);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[i] = quant4(t[4 * i], t[4 * i + 1], t[4 * i + 2], t[4 * i + 3]) & mask;
+}
+// One 16-channel chunk of the fused layer boundary with an activation (`ent` as in next_slab16)
+__device__ __forceinline__ void next_slab16_act(const GemmParams &p, int ent, const uint32_t *r, const float *alpha16, const float *beta16, uint32_t *out)
+{
+    float lo = -128.f, hi = 127.f, v[16];
+    uint32_t mask = 0xffffffffu;
+    if ((ent & 0xffffff) * 16 < p.next_K_lo) {
+        const int sft = ent >> 24;
+        hi = (float)(8 << sft) - 1.f;
+        lo = -(float)(8 << sft);
+        mask = ((0xffu << sft) & 0xffu) * 0x01010101u;
+    }
+    finish16_act(p, r, alpha16, beta16, nullptr, v);
+    quantize16_f32(p, v, lo, hi, mask, out);
+}
 __device__ __forceinline__ void st_global_128(void *p, uint32_t a, uint32_t b, uint32_t c, uint32_t d)
 {
     asm volatile("st.global.v4.b32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
@@ -359,7 +409,7 @@ struct EpilogueCtx {
 // 8 four-byte columns) and leave through tiled bulk stores.  The first half is stored before the accumulator goes back; against the one
 // kernel for all outputs, which read the whole slice first, no shape is slower for it (int8, GEMM alone: ViT-B QKV 19.2 -> 18.0 us,
 // fc2 22.3 -> 21.7, ViT-L fc2 70-83 and 70-86 us under the power cap).
-template <int CG, int MODE, bool SPLIT, int KIND>
+template <int CG, int MODE, bool SPLIT, int KIND, bool ACT = false>
 __device__ __forceinline__ void epilogue_role(const GemmParams &p, const EpilogueCtx &x, int quad, int part, int lane)
 {
     constexpr bool kPatch = KIND == 2, kGrid = KIND >= 2;
@@ -381,6 +431,11 @@ __device__ __forceinline__ void epilogue_role(const GemmParams &p, const Epilogu
     PROF_DECL(prof_ld);
     PROF_DECL(prof_math);
     PROF_T0(prof_start);
+    // this lane's residual at output channel n (rows outside Y have none)
+    const int res_bytes = p.res_dtype == FLEXIQ_DTYPE_F32 ? 4 : 2;
+    auto residual = [&](long long r, int n) -> const void * {
+        return p.res && r < p.M ? static_cast<const char *>(p.res) + ((size_t)r * p.N + n) * res_bytes : nullptr;
+    };
     const int passes = 4 / x.parts;              // 1 with sixteen epilogue warps, 2 with eight
     // Patch mode keeps four accumulators, tile ti in accumulator ti mod 4.  With 64-column tiles only column
     // slots 0 and 1 of a lane quadrant have columns, so slots 2 and 3 take the odd tiles instead of idling.
@@ -495,7 +550,18 @@ __device__ __forceinline__ void epilogue_role(const GemmParams &p, const Epilogu
                             // is lowered when it lies below the next layer's max_4bit_ch
 #pragma unroll
                             for (int g = 0; g < 2; ++g)
-                                if (g == 0 || both) next_slab16(p, (h ? ents[2 + g] : ents[g]), r + 16 * g, fac + 16 * g, fac + 64 + 16 * g, w + 4 * g);
+                                if (g == 0 || both) {
+                                    if (ACT) next_slab16_act(p, (h ? ents[2 + g] : ents[g]), r + 16 * g, fac + 16 * g, fac + 64 + 16 * g, w + 4 * g);
+                                    else next_slab16(p, (h ? ents[2 + g] : ents[g]), r + 16 * g, fac + 16 * g, fac + 64 + 16 * g, w + 4 * g);
+                                }
+                        } else if (ACT) {
+#pragma unroll
+                            for (int g = 0; g < 2; ++g)
+                                if (g == 0 || both) {
+                                    float v[16];
+                                    finish16_act(p, r + 16 * g, fac + 16 * g, fac + 64 + 16 * g, residual(row, n + 16 * g), v);
+                                    quantize16_f32(p, v, -128.f, 127.f, 0xffffffffu, w + 4 * g);
+                                }
                         } else {
                             finish16<FLEXIQ_OUT_REQUANT_I8>(r, fac, fac + 64, w);
                             if (both) finish16<FLEXIQ_OUT_REQUANT_I8>(r + 16, fac + 16, fac + 64 + 16, w + 4);
@@ -525,7 +591,8 @@ __device__ __forceinline__ void epilogue_role(const GemmParams &p, const Epilogu
                         const int n = nw + 32 * h + 16 * g;
                         if (n < p.N && row0 < p.M) {   // warp-uniform
                             uint32_t w[16], hw[8];
-                            finish16<FLEXIQ_OUT_DEQUANT_F32>(r + 16 * g, fac + 16 * g, fac + 64 + 16 * g, w);
+                            if (ACT) finish16_act(p, r + 16 * g, fac + 16 * g, fac + 64 + 16 * g, residual(row, n), reinterpret_cast<float *>(w));
+                            else finish16<FLEXIQ_OUT_DEQUANT_F32>(r + 16 * g, fac + 16 * g, fac + 64 + 16 * g, w);
 #pragma unroll
                             for (int q = 0; q < 8; ++q)
                                 hw[q] = pack2_f16<MODE == FLEXIQ_OUT_DEQUANT_BF16>(__uint_as_float(w[2 * q]), __uint_as_float(w[2 * q + 1]));
@@ -551,7 +618,8 @@ __device__ __forceinline__ void epilogue_role(const GemmParams &p, const Epilogu
                         const int n = nw + 32 * h + 16 * g;
                         if (n < p.N && row0 < p.M) {   // warp-uniform
                             uint32_t w[16];
-                            finish16<MODE>(r + 16 * g, fac + 16 * g, fac + 64 + 16 * g, w);
+                            if (ACT) finish16_act(p, r + 16 * g, fac + 16 * g, fac + 64 + 16 * g, residual(row, n), reinterpret_cast<float *>(w));
+                            else finish16<MODE>(r + 16 * g, fac + 16 * g, fac + 64 + 16 * g, w);
                             const uint32_t dst = x.store_stage + (uint32_t)lane * 32u;
                             const uint32_t sw16 = ((uint32_t)lane >> 2 & 1u) << 4;
 #pragma unroll
@@ -584,7 +652,8 @@ __device__ __forceinline__ void epilogue_role(const GemmParams &p, const Epilogu
                         for (int g = 0; g < 2; ++g) {
                             if (g == 0 || second) {
                                 pos[g] = (h ? ents[2 + g] : ents[g]) & 0xffffff;
-                                next_slab16(p, (h ? ents[2 + g] : ents[g]), r + 16 * g, fac + 16 * g, fac + 64 + 16 * g, w + 4 * g);
+                                if (ACT) next_slab16_act(p, (h ? ents[2 + g] : ents[g]), r + 16 * g, fac + 16 * g, fac + 64 + 16 * g, w + 4 * g);
+                                else next_slab16(p, (h ? ents[2 + g] : ents[g]), r + 16 * g, fac + 16 * g, fac + 64 + 16 * g, w + 4 * g);
                             }
                         }
                         if (second && wide && pos[1] == pos[0] + 1 && (pos[0] & 1) == 0) st_global_256(srow + pos[0] * 16, w);
@@ -1247,14 +1316,16 @@ mixed_gemm_kernel(const __grid_constant__ CUtensorMap mapA_lo, const __grid_cons
             x.map_y = &mapY; x.map_y16 = &mapY16;
             x.first_tile = first_tile; x.tile_step = tile_step; x.num_tiles = num_tiles;
             x.parts = kEpiWarps / 4; x.arrivals_on = 1;
-            if constexpr (OUT == kKindI8) epilogue_role<CG, FLEXIQ_OUT_REQUANT_I8, SPLIT, KIND>(p, x, warp & 3, e >> 2, lane);
-            else if constexpr (OUT == kKindNext) epilogue_role<CG, kOutNextSlab, SPLIT, KIND>(p, x, warp & 3, e >> 2, lane);
-            else if constexpr (OUT == kKindScatter) epilogue_role<CG, kOutScatter, SPLIT, KIND>(p, x, warp & 3, e >> 2, lane);
-            else if constexpr (OUT == kKindHalf) {
-                if (p.out_mode == FLEXIQ_OUT_DEQUANT_F16) epilogue_role<CG, FLEXIQ_OUT_DEQUANT_F16, SPLIT, KIND>(p, x, warp & 3, e >> 2, lane);
-                else epilogue_role<CG, FLEXIQ_OUT_DEQUANT_BF16, SPLIT, KIND>(p, x, warp & 3, e >> 2, lane);
+            constexpr bool kAct = OUT >= kActKinds;
+            constexpr int kOut = kAct ? OUT - kActKinds : OUT;
+            if constexpr (kOut == kKindI8) epilogue_role<CG, FLEXIQ_OUT_REQUANT_I8, SPLIT, KIND, kAct>(p, x, warp & 3, e >> 2, lane);
+            else if constexpr (kOut == kKindNext) epilogue_role<CG, kOutNextSlab, SPLIT, KIND, kAct>(p, x, warp & 3, e >> 2, lane);
+            else if constexpr (kOut == kKindScatter) epilogue_role<CG, kOutScatter, SPLIT, KIND, kAct>(p, x, warp & 3, e >> 2, lane);
+            else if constexpr (kOut == kKindHalf) {
+                if (p.out_mode == FLEXIQ_OUT_DEQUANT_F16) epilogue_role<CG, FLEXIQ_OUT_DEQUANT_F16, SPLIT, KIND, kAct>(p, x, warp & 3, e >> 2, lane);
+                else epilogue_role<CG, FLEXIQ_OUT_DEQUANT_BF16, SPLIT, KIND, kAct>(p, x, warp & 3, e >> 2, lane);
             } else {
-                if (p.out_mode == FLEXIQ_OUT_DEQUANT_F32) epilogue_role<CG, FLEXIQ_OUT_DEQUANT_F32, SPLIT, KIND>(p, x, warp & 3, e >> 2, lane);
+                if (kAct || p.out_mode == FLEXIQ_OUT_DEQUANT_F32) epilogue_role<CG, FLEXIQ_OUT_DEQUANT_F32, SPLIT, KIND, kAct>(p, x, warp & 3, e >> 2, lane);
                 else epilogue_role<CG, FLEXIQ_OUT_ACC_I32, SPLIT, KIND>(p, x, warp & 3, e >> 2, lane);
             }
         } else if (PK && warp < 2 + kNumWorkWarps) {
@@ -1705,9 +1776,12 @@ static int sync_straddle(Layer *L, cudaStream_t st)
     return FLEXIQ_OK;
 }
 
+// What the epilogue does beyond bias and scale; NULL for the calls without.
+struct EpilogueOps { int act; const void *res; int res_dtype, res_order; };
+
 static int run_mixed(Layer *L, const uint8_t *X4, const int8_t *X8, const uint8_t *x_shift, long long M, int Nb, int H,
                      int W, float x_scale, float y_scale, int out_mode, void *Y, cudaStream_t st,
-                     const Layer *next = nullptr, int relu = 0, int out_order = 0)
+                     Layer *next = nullptr, int relu = 0, int out_order = 0, const EpilogueOps *ops = nullptr)
 {
     if (next) {
         // fused layer boundary: Y is the next layer's masked slab, y_scale its activation scale
@@ -1724,6 +1798,21 @@ static int run_mixed(Layer *L, const uint8_t *X4, const int8_t *X8, const uint8_
         return set_error(FLEXIQ_ERR_INVALID_ARG, "unknown out_mode %d", out_mode);
     if ((out_mode == FLEXIQ_OUT_REQUANT_I8 || next) && !(y_scale > 0.0f))
         return set_error(FLEXIQ_ERR_INVALID_ARG, "y_scale %g must be positive", (double)y_scale);
+    if (ops) {
+        if (out_mode == FLEXIQ_OUT_ACC_I32) return set_error(FLEXIQ_ERR_INVALID_ARG, "raw accumulators take neither an activation nor a residual");
+        if (!act_known(ops->act)) return set_error(FLEXIQ_ERR_INVALID_ARG, "unknown act %d", ops->act);
+        if (ops->res) {
+            if (ops->res_dtype != FLEXIQ_DTYPE_F32 && ops->res_dtype != FLEXIQ_DTYPE_F16 && ops->res_dtype != FLEXIQ_DTYPE_BF16)
+                return set_error(FLEXIQ_ERR_INVALID_ARG, "residual_dtype %d is not F32, F16 or BF16", ops->res_dtype);
+            if (ops->res_order != FLEXIQ_RESIDUAL_AFTER_ACT && ops->res_order != FLEXIQ_RESIDUAL_BEFORE_ACT)
+                return set_error(FLEXIQ_ERR_INVALID_ARG, "unknown residual_order %d", ops->res_order);
+            if (reinterpret_cast<uintptr_t>(ops->res) & 15) return set_error(FLEXIQ_ERR_INVALID_ARG, "residual_dev must be 16-byte aligned");
+            const int same = out_mode == FLEXIQ_OUT_DEQUANT_F32 ? FLEXIQ_DTYPE_F32 : out_mode == FLEXIQ_OUT_DEQUANT_F16 ? FLEXIQ_DTYPE_F16
+                           : out_mode == FLEXIQ_OUT_DEQUANT_BF16 ? FLEXIQ_DTYPE_BF16 : -1;
+            if (ops->res == Y && ops->res_dtype != same)
+                return set_error(FLEXIQ_ERR_INVALID_ARG, "Y_dev is residual_dev, which needs an output of the residual's type");
+        }
+    }
     if (M == 0) return FLEXIQ_OK;
     const int C_lo = L->K_lo, C_hi = L->C - C_lo;
     if (!Y) return set_error(FLEXIQ_ERR_INVALID_ARG, "Y_dev is NULL");
@@ -1785,11 +1874,19 @@ static int run_mixed(Layer *L, const uint8_t *X4, const int8_t *X8, const uint8_
     }
     p.out_mode = out_mode; p.Y = Y;
     if (next) { p.next_ent = out_order == FLEXIQ_ORDER_NEXT_SLAB ? next->chunk_ent_slab : next->chunk_ent; p.next_K_lo = next->K_lo; p.relu = relu != 0; }
+    if (ops) {
+        p.act = ops->act; p.res = ops->res; p.res_dtype = ops->res_dtype; p.res_first = ops->res_order == FLEXIQ_RESIDUAL_BEFORE_ACT;
+        p.q_scale = y_scale;
+        if (next) p.quot = quotient_plan(next, y_scale, FLEXIQ_DTYPE_F32);
+        else if (out_mode == FLEXIQ_OUT_REQUANT_I8) p.quot = plan_quotient(y_scale, FLEXIQ_DTYPE_F32);
+    }
     // The per-output-channel factors depend on the call's scales.  The handle keeps a few factor tables, each
     // written once for one (kind, S_x, S_y) and never changed while anything may still depend on it, so a
     // table that a captured graph reads (or writes) stays what that graph expects whatever runs in between.
-    // The fused boundary re-quantizes with the REQUANT factors; the three floating-point outputs share theirs.
-    const int fmode = next ? FLEXIQ_OUT_REQUANT_I8
+    // The fused boundary re-quantizes with the REQUANT factors; the three floating-point outputs share theirs, and so does whatever an
+    // activation or a residual follows.
+    const int fmode = ops ? FLEXIQ_OUT_DEQUANT_F32
+                    : next ? FLEXIQ_OUT_REQUANT_I8
                            : ((out_mode == FLEXIQ_OUT_DEQUANT_F16 || out_mode == FLEXIQ_OUT_DEQUANT_BF16) ? FLEXIQ_OUT_DEQUANT_F32 : out_mode);
     if (fmode != FLEXIQ_OUT_ACC_I32) {
         const unsigned long long cap = stream_capture_id(st);
@@ -1976,14 +2073,21 @@ static int run_mixed(Layer *L, const uint8_t *X4, const int8_t *X8, const uint8_
     // second accumulator's extra read in the epilogue would only cost (measured: +4 to +6 % on short-K shapes).
     const bool split = !packed && !patch && !stream && bn <= 128 && p.tps == 1 && p.T * (p.nb_lo + p.nb_hi) >= 8 &&
                        (long long)p.m_tiles * p.n_tiles <= sms / cg;
-    if (next) record_slab(const_cast<Layer *>(next), Y, next->K_lo);   // the fused boundary writes the next layer's slab at its current ratio
+    if (next) record_slab(next, Y, next->K_lo);   // the fused boundary writes the next layer's slab at its current ratio
     // multi-tap stages hold every channel in one K block: the whole weight operand is one of the three forms
     const bool one_block = (p.tps > 1 && !stream) || patch;
     if (one_block && b_whole == 2) p.b_tap_step = p.BK;
     LaunchMaps maps{a_lo, a_hi, packed ? L->map_w4[bi] : L->map_w8m[bi], L->map_w8[bi], packed ? L->map_w8[bi] : L->map_wst[bi], y_map, y_map16};
     if (one_block && b_whole != 0) maps.b_hi = b_whole == 1 ? L->map_w8m[bi] : L->map_wst[bi];
     const LaunchForm form{cg, packed, patch, stream, conv_kind, split};
-    switch (out_kind(out_mode, staged)) {
+    if (ops) switch (out_kind(out_mode, staged)) {
+        case kKindI8: rc = launch_form<kKindActI8>(form, maps, p, sms, st); break;
+        case kKindScatter: rc = launch_form<kKindActScatter>(form, maps, p, sms, st); break;
+        case kKindNext: rc = launch_form<kKindActNext>(form, maps, p, sms, st); break;
+        case kKindHalf: rc = launch_form<kKindActHalf>(form, maps, p, sms, st); break;
+        default: rc = launch_form<kKindActWord>(form, maps, p, sms, st); break;
+    }
+    else switch (out_kind(out_mode, staged)) {
         case kKindI8: rc = launch_form<kKindI8>(form, maps, p, sms, st); break;
         case kKindScatter: rc = launch_form<kKindScatter>(form, maps, p, sms, st); break;
         case kKindNext: rc = launch_form<kKindNext>(form, maps, p, sms, st); break;
@@ -2055,6 +2159,78 @@ extern "C" int flexiq_mixed_conv_to_slab(flexiq_layer_t layer, const uint8_t *X4
     if (P <= 0 || Q <= 0) return set_error(FLEXIQ_ERR_INVALID_ARG, "filter does not fit the padded input");
     return run_mixed(L, X4_dev, X8_dev, x_shift_dev, (long long)Nb * P * Q, Nb, H, W, x_scale, next_x_scale, 0, next_X4_dev,
                      reinterpret_cast<cudaStream_t>(stream), Nx, relu, out_order);
+}
+
+// The live handle behind `layer` (of the kind asked for), or NULL with the error set.
+static Layer *layer_of_kind(flexiq_layer_t layer, bool conv)
+{
+    Layer *L = as_layer(layer);
+    if (!L) set_error(FLEXIQ_ERR_INVALID_ARG, "not a live flexiq layer handle");
+    else if ((L->is_conv != 0) != conv) {
+        set_error(FLEXIQ_ERR_INVALID_ARG, conv ? "layer is linear: use the mixed_gemm form" : "layer is a convolution: use the mixed_conv form");
+        return nullptr;
+    }
+    return L;
+}
+// Output pixels of a convolution call, or -1 with the error set.
+static long long conv_rows(const Layer *L, int Nb, int H, int W)
+{
+    if (Nb < 0 || H <= 0 || W <= 0) { set_error(FLEXIQ_ERR_INVALID_ARG, "bad activation shape Nb=%d H=%d W=%d", Nb, H, W); return -1; }
+    const long long P = (H + 2ll * L->pad - L->R), Q = (W + 2ll * L->pad - L->S);
+    if (P < 0 || Q < 0) { set_error(FLEXIQ_ERR_INVALID_ARG, "filter does not fit the padded input"); return -1; }
+    return (long long)Nb * (P / L->stride + 1) * (Q / L->stride + 1);
+}
+
+extern "C" int flexiq_mixed_gemm_act(flexiq_layer_t layer, const uint8_t *X4_dev, const int8_t *X8_dev, const uint8_t *x_shift_dev, int64_t M,
+                                     float x_scale, float y_scale, int act, const void *residual_dev, int residual_dtype, int residual_order,
+                                     int out_mode, void *Y_dev, void *stream)
+{
+    Layer *L = layer_of_kind(layer, false);
+    if (!L) return FLEXIQ_ERR_INVALID_ARG;
+    if (M < 0) return set_error(FLEXIQ_ERR_INVALID_ARG, "M = %lld is negative", (long long)M);
+    const EpilogueOps ops{act, residual_dev, residual_dtype, residual_order};
+    return run_mixed(L, X4_dev, X8_dev, x_shift_dev, M, 0, 0, 0, x_scale, y_scale, out_mode, Y_dev, reinterpret_cast<cudaStream_t>(stream),
+                     nullptr, 0, 0, &ops);
+}
+
+extern "C" int flexiq_mixed_conv_act(flexiq_layer_t layer, const uint8_t *X4_dev, const int8_t *X8_dev, const uint8_t *x_shift_dev, int Nb, int H,
+                                     int W, float x_scale, float y_scale, int act, const void *residual_dev, int residual_dtype,
+                                     int residual_order, int out_mode, void *Y_dev, void *stream)
+{
+    Layer *L = layer_of_kind(layer, true);
+    if (!L) return FLEXIQ_ERR_INVALID_ARG;
+    const long long M = conv_rows(L, Nb, H, W);
+    if (M < 0) return FLEXIQ_ERR_INVALID_ARG;
+    const EpilogueOps ops{act, residual_dev, residual_dtype, residual_order};
+    return run_mixed(L, X4_dev, X8_dev, x_shift_dev, M, Nb, H, W, x_scale, y_scale, out_mode, Y_dev, reinterpret_cast<cudaStream_t>(stream),
+                     nullptr, 0, 0, &ops);
+}
+
+extern "C" int flexiq_mixed_gemm_act_to_slab(flexiq_layer_t layer, const uint8_t *X4_dev, const int8_t *X8_dev, const uint8_t *x_shift_dev, int64_t M,
+                                             float x_scale, flexiq_layer_t next_layer, float next_x_scale, int act, int out_order,
+                                             uint8_t *next_X4_dev, void *stream)
+{
+    Layer *L = layer_of_kind(layer, false), *Nx = as_layer(next_layer);
+    if (!L) return FLEXIQ_ERR_INVALID_ARG;
+    if (!Nx) return set_error(FLEXIQ_ERR_INVALID_ARG, "not a live flexiq layer handle");
+    if (M < 0) return set_error(FLEXIQ_ERR_INVALID_ARG, "M = %lld is negative", (long long)M);
+    const EpilogueOps ops{act, nullptr, 0, 0};
+    return run_mixed(L, X4_dev, X8_dev, x_shift_dev, M, 0, 0, 0, x_scale, next_x_scale, 0, next_X4_dev, reinterpret_cast<cudaStream_t>(stream),
+                     Nx, 0, out_order, &ops);
+}
+
+extern "C" int flexiq_mixed_conv_act_to_slab(flexiq_layer_t layer, const uint8_t *X4_dev, const int8_t *X8_dev, const uint8_t *x_shift_dev, int Nb,
+                                             int H, int W, float x_scale, flexiq_layer_t next_layer, float next_x_scale, int act, int out_order,
+                                             uint8_t *next_X4_dev, void *stream)
+{
+    Layer *L = layer_of_kind(layer, true), *Nx = as_layer(next_layer);
+    if (!L) return FLEXIQ_ERR_INVALID_ARG;
+    if (!Nx) return set_error(FLEXIQ_ERR_INVALID_ARG, "not a live flexiq layer handle");
+    const long long M = conv_rows(L, Nb, H, W);
+    if (M < 0) return FLEXIQ_ERR_INVALID_ARG;
+    const EpilogueOps ops{act, nullptr, 0, 0};
+    return run_mixed(L, X4_dev, X8_dev, x_shift_dev, M, Nb, H, W, x_scale, next_x_scale, 0, next_X4_dev, reinterpret_cast<cudaStream_t>(stream),
+                     Nx, 0, out_order, &ops);
 }
 
 extern "C" int flexiq_choose_tile(int64_t M, int N, int k_blocks, int block_k, int sm_count, int *cta_group_out, int *tile_n_out)

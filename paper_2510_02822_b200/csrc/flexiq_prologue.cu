@@ -577,7 +577,7 @@ static int static_scratch_address(unsigned **out)
 }
 
 // The plan of the layer's scale (plan_quotient takes about half a microsecond for 16-bit inputs), one per input type.
-static QuotientPlan quotient_plan(Layer *L, float S, int dtype)
+QuotientPlan quotient_plan(Layer *L, float S, int dtype)
 {
     Layer::Quotient &k = L->quotient[dtype];
     if (k.S != S) {

@@ -336,6 +336,215 @@ PyObject *calls_mixed_conv_to_slab(PyObject *self, PyObject *const *args, Py_ssi
     });
 }
 
+// A tensor the library may take as it is: contiguous, on the layer's device, of this many elements.  (Others are refused by the general path.)
+void *plain(const at::Tensor &t, long long count, int device)
+{
+    if (!t.is_cuda() || t.device().index() != device || !t.is_contiguous() || t.numel() != count) throw Refused{};
+    return t.data_ptr();
+}
+// the same for a slab of at least `bytes` bytes: the caller's, or the next layer's own (new reference)
+PyObject *checked_slab(PyObject *slab, Calls *next, long long M, void **ptr)
+{
+    if (M < 0) throw Refused{};
+    if (slab != Py_None) {
+        const at::Tensor &t = tensor(slab);
+        if (!t.is_cuda() || t.device().index() != next->device || !t.is_contiguous() || t.element_size() != 1 || t.numel() < M * next->K) throw Refused{};
+    }
+    return next_slab(slab, next, M, ptr);
+}
+struct Epilogue { int act, dtype = 0, order, mode; float y_scale; void *residual = nullptr, *y = nullptr; Owned out; };
+// act, out_mode, residual, residual_order, y_scale, Y: the arguments behind the layer's own, checked, and the output
+void epilogue_args(Calls *c, PyObject *const *args, at::IntArrayRef size, Epilogue *e)
+{
+    e->act = whole32(args[0]);
+    e->mode = whole32(args[1]);
+    e->order = whole32(args[3]);
+    e->y_scale = number(args[4]);
+    long long count = 1;
+    for (const long long d : size) count *= d;
+    const at::ScalarType type = out_type(e->mode);
+    if (args[2] != Py_None) {
+        const at::Tensor &r = tensor(args[2]);
+        e->residual = plain(r, count, c->device);
+        e->dtype = dtype_code(r);
+    }
+    if (args[5] == Py_None) {
+        const at::Tensor t = device_empty(c, size, type);
+        e->y = t.data_ptr();
+        if (!(e->out.o = THPVariable_Wrap(t))) throw Refused{};
+    } else {
+        const at::Tensor &t = tensor(args[5]);
+        if (t.scalar_type() != type) throw Refused{};
+        e->y = plain(t, count, c->device);
+        e->out.o = Py_NewRef(args[5]);
+    }
+}
+
+// mixed_gemm_act(x4, x8, M, x_scale, x_shift, act, out_mode, residual, residual_order, y_scale, Y) -> Y
+PyObject *calls_mixed_gemm_act(PyObject *self, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        if (n != 11) throw Refused{};
+        Calls *c = reinterpret_cast<Calls *>(self);
+        const void *x4 = pointer(args[0]), *x8 = pointer(args[1]), *xs = pointer(args[4]);
+        const long long M = whole(args[2]);
+        const float x_scale = number(args[3]);
+        if (M < 0) throw Refused{};
+        Epilogue e;
+        epilogue_args(c, args + 5, {M, c->N}, &e);
+        void *st = current_stream();
+        const int rc = released([&] {
+            return flexiq_mixed_gemm_act(c->h, static_cast<const uint8_t *>(x4), static_cast<const int8_t *>(x8), static_cast<const uint8_t *>(xs), M, x_scale,
+                                         e.y_scale, e.act, e.residual, e.dtype, e.order, e.mode, e.y, st);
+        });
+        return finish(rc, e.out.release());
+    });
+}
+
+// mixed_conv_act(x4, x8, Nb, H, W, x_scale, x_shift, act, out_mode, residual, residual_order, y_scale, Y) -> Y
+PyObject *calls_mixed_conv_act(PyObject *self, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        if (n != 13) throw Refused{};
+        Calls *c = reinterpret_cast<Calls *>(self);
+        const void *x4 = pointer(args[0]), *x8 = pointer(args[1]), *xs = pointer(args[6]);
+        const int Nb = whole32(args[2]), H = whole32(args[3]), W = whole32(args[4]);
+        const float x_scale = number(args[5]);
+        long long P, Q;
+        out_size(c, H, W, &P, &Q);
+        if (Nb < 0) throw Refused{};
+        Epilogue e;
+        epilogue_args(c, args + 7, {Nb, P, Q, c->N}, &e);
+        void *st = current_stream();
+        const int rc = released([&] {
+            return flexiq_mixed_conv_act(c->h, static_cast<const uint8_t *>(x4), static_cast<const int8_t *>(x8), static_cast<const uint8_t *>(xs), Nb, H, W, x_scale,
+                                         e.y_scale, e.act, e.residual, e.dtype, e.order, e.mode, e.y, st);
+        });
+        return finish(rc, e.out.release());
+    });
+}
+
+// mixed_gemm_act_to_slab(x4, x8, M, x_scale, next, next_x_scale, act, slab, x_shift, out_order) -> slab
+PyObject *calls_mixed_gemm_act_to_slab(PyObject *self, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        if (n != 10) throw Refused{};
+        Calls *c = reinterpret_cast<Calls *>(self), *next = calls_of(args[4]);
+        const void *x4 = pointer(args[0]), *x8 = pointer(args[1]), *xs = pointer(args[8]);
+        const long long M = whole(args[2]);
+        const float x_scale = number(args[3]), next_scale = number(args[5]);
+        const int act = whole32(args[6]), order = whole32(args[9]);
+        void *out;
+        PyObject *slab = checked_slab(args[7], next, M, &out);
+        void *st = current_stream();
+        return finish(released([&] {
+            return flexiq_mixed_gemm_act_to_slab(c->h, static_cast<const uint8_t *>(x4), static_cast<const int8_t *>(x8), static_cast<const uint8_t *>(xs),
+                                                 M, x_scale, next->h, next_scale, act, order, static_cast<uint8_t *>(out), st);
+        }), slab);
+    });
+}
+
+// mixed_conv_act_to_slab(x4, x8, Nb, H, W, x_scale, next, next_x_scale, act, slab, x_shift, out_order) -> slab
+PyObject *calls_mixed_conv_act_to_slab(PyObject *self, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        if (n != 12) throw Refused{};
+        Calls *c = reinterpret_cast<Calls *>(self), *next = calls_of(args[6]);
+        const void *x4 = pointer(args[0]), *x8 = pointer(args[1]), *xs = pointer(args[10]);
+        const int Nb = whole32(args[2]), H = whole32(args[3]), W = whole32(args[4]);
+        const float x_scale = number(args[5]), next_scale = number(args[7]);
+        const int act = whole32(args[8]), order = whole32(args[11]);
+        long long P, Q;
+        out_size(c, H, W, &P, &Q);
+        void *out;
+        PyObject *slab = checked_slab(args[9], next, Nb * P * Q, &out);
+        void *st = current_stream();
+        return finish(released([&] {
+            return flexiq_mixed_conv_act_to_slab(c->h, static_cast<const uint8_t *>(x4), static_cast<const int8_t *>(x8), static_cast<const uint8_t *>(xs),
+                                                 Nb, H, W, x_scale, next->h, next_scale, act, order, static_cast<uint8_t *>(out), st);
+        }), slab);
+    });
+}
+
+struct Norm { at::Tensor scratch; long long Nb, P; int C, groups, dtype, act, device; float eps; const float *gamma, *beta; void *x; };
+// X, groups, gamma, beta, eps, act
+void norm_args(PyObject *const *args, Norm *a)
+{
+    const at::Tensor &X = tensor(args[0]);
+    a->groups = whole32(args[1]);
+    a->eps = number(args[4]);
+    a->act = whole32(args[5]);
+    if (!X.is_cuda() || X.dim() < 2 || !X.is_contiguous() || X.size(-1) > INT32_MAX) throw Refused{};
+    a->dtype = dtype_code(X);
+    a->device = X.device().index();
+    if (a->device != c10::cuda::current_device()) throw Refused{};
+    a->Nb = X.size(0);
+    a->C = (int)X.size(-1);
+    a->P = 1;
+    for (int64_t d = 1; d + 1 < X.dim(); ++d) a->P *= X.size(d);
+    const float *p[2];
+    for (int i = 0; i < 2; ++i) {
+        p[i] = nullptr;
+        if (args[2 + i] == Py_None) continue;
+        const at::Tensor &t = tensor(args[2 + i]);
+        if (t.scalar_type() != at::kFloat || !t.is_cuda() || t.device().index() != a->device || !t.is_contiguous() || t.numel() != a->C) throw Refused{};
+        p[i] = t.data_ptr<float>();
+    }
+    a->gamma = p[0];
+    a->beta = p[1];
+    a->x = X.data_ptr();
+    int64_t bytes = 0;
+    if (flexiq_group_norm_scratch(a->dtype, a->Nb, a->P, a->C, a->groups, &bytes) != FLEXIQ_OK) throw Refused{};
+    if (bytes) a->scratch = at::detail::empty_cuda({bytes}, at::kByte, X.device(), std::nullopt);
+}
+
+// group_norm(X, groups, gamma, beta, eps, act, y_dtype code, Y) -> Y
+PyObject *group_norm(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        if (n != 8) throw Refused{};
+        Norm a;
+        norm_args(args, &a);
+        const at::Tensor &X = tensor(args[0]);
+        const int code = whole32(args[6]);
+        const at::ScalarType type = code == FLEXIQ_DTYPE_F32 ? at::kFloat : code == FLEXIQ_DTYPE_F16 ? at::kHalf : code == FLEXIQ_DTYPE_BF16 ? at::kBFloat16 : throw Refused{};
+        Owned out;
+        void *y;
+        if (args[7] == Py_None) {
+            const at::Tensor t = at::detail::empty_cuda(X.sizes(), type, X.device(), std::nullopt);
+            y = t.data_ptr();
+            if (!(out.o = THPVariable_Wrap(t))) throw Refused{};
+        } else {
+            const at::Tensor &t = tensor(args[7]);
+            if (t.scalar_type() != type || !t.is_cuda() || t.device() != X.device() || !t.is_contiguous() || t.numel() != X.numel()) throw Refused{};
+            y = t.data_ptr();
+            out.o = Py_NewRef(args[7]);
+        }
+        void *st = current_stream(), *scratch = a.scratch.defined() ? a.scratch.data_ptr() : nullptr;
+        const int rc = released([&] { return flexiq_group_norm(a.x, a.dtype, a.Nb, a.P, a.C, a.groups, a.gamma, a.beta, a.eps, a.act, code, y, scratch, st); });
+        return finish(rc, out.release());
+    });
+}
+
+// group_norm_to_slab(X, groups, gamma, beta, eps, act, x_scale, slab) -> slab
+PyObject *calls_group_norm_to_slab(PyObject *self, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        if (n != 8) throw Refused{};
+        Calls *c = reinterpret_cast<Calls *>(self);
+        Norm a;
+        norm_args(args, &a);
+        if (a.C != c->K || a.device != c->device) throw Refused{};
+        const float scale = number(args[6]);
+        void *out;
+        PyObject *slab = checked_slab(args[7], c, a.Nb * a.P, &out);
+        void *st = current_stream(), *scratch = a.scratch.defined() ? a.scratch.data_ptr() : nullptr;
+        return finish(released([&] {
+            return flexiq_group_norm_to_slab(c->h, a.x, a.dtype, a.Nb, a.P, a.groups, a.gamma, a.beta, a.eps, a.act, scale, static_cast<uint8_t *>(out), scratch, st);
+        }), slab);
+    });
+}
+
 PyObject *calls_set_lowbit_ratio(PyObject *self, PyObject *ratio)
 {
     return guarded([&]() -> PyObject * {
@@ -421,6 +630,11 @@ PyMethodDef calls_methods[] = {
     {"mixed_conv", (PyCFunction)(void (*)(void))calls_mixed_conv, METH_FASTCALL, nullptr},
     {"mixed_gemm_to_slab", (PyCFunction)(void (*)(void))calls_mixed_gemm_to_slab, METH_FASTCALL, nullptr},
     {"mixed_conv_to_slab", (PyCFunction)(void (*)(void))calls_mixed_conv_to_slab, METH_FASTCALL, nullptr},
+    {"mixed_gemm_act", (PyCFunction)(void (*)(void))calls_mixed_gemm_act, METH_FASTCALL, nullptr},
+    {"mixed_conv_act", (PyCFunction)(void (*)(void))calls_mixed_conv_act, METH_FASTCALL, nullptr},
+    {"mixed_gemm_act_to_slab", (PyCFunction)(void (*)(void))calls_mixed_gemm_act_to_slab, METH_FASTCALL, nullptr},
+    {"mixed_conv_act_to_slab", (PyCFunction)(void (*)(void))calls_mixed_conv_act_to_slab, METH_FASTCALL, nullptr},
+    {"group_norm_to_slab", (PyCFunction)(void (*)(void))calls_group_norm_to_slab, METH_FASTCALL, nullptr},
     {"set_lowbit_ratio", calls_set_lowbit_ratio, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
@@ -575,6 +789,7 @@ PyObject *set_error_class(PyObject *, PyObject *cls)
 PyMethodDef module_methods[] = {
     {"static_preparation", (PyCFunction)(void (*)(void))static_preparation, METH_FASTCALL, nullptr},
     {"select_groups", (PyCFunction)(void (*)(void))select_groups, METH_FASTCALL, nullptr},
+    {"group_norm", (PyCFunction)(void (*)(void))group_norm, METH_FASTCALL, nullptr},
     {"sq_distance_i8", (PyCFunction)(void (*)(void))sq_distance, METH_FASTCALL, nullptr},
     {"set_error_class", set_error_class, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr},
