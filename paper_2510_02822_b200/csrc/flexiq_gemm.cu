@@ -44,6 +44,11 @@ constexpr int kFactorsPerWarp = 512;                  // alpha[64] | beta[64] of
 constexpr int kMaxStages = 8;
 constexpr int kStoreStagePerWarp = 1024;              // 32 rows x 32 int8 columns staged for a tiled bulk store
 constexpr int kSmemBytes = kStageRegion + kNumWorkWarps * (kFactorsPerWarp + kStoreStagePerWarp) + 256;
+// With a residual: two kilobytes more a warp behind the barriers, and as much less ring as the SM's 227 KB do not hold besides.
+constexpr int kResPerWarp = 2048;                     // 32 rows x 64 bytes
+constexpr int kStageRegionRes = 174080;
+constexpr int kSmemBytesRes = kStageRegionRes + kNumWorkWarps * (kFactorsPerWarp + kStoreStagePerWarp + kResPerWarp) + 256;
+static_assert(kSmemBytesRes <= 232448, "shared memory of a block");
 
 // Internal epilogue mode of the fused layer boundary: the int8 result goes straight into the
 // next layer's masked slab (its channel order, its low groups lowered).
@@ -54,9 +59,10 @@ constexpr int kOutScatter = 6;
 // A kernel serves one kind of output.  One kernel for all of them spilled registers in every epilogue (ptxas, per thread: 160 bytes stored
 // and 180 loaded in the plain CTA pair, 108 and 244 in the single CTA, none in either now), and the epilogue is as long as the mainloop
 // at short K.  Packed path, 768 -> 3072 at 12,608 rows 60.7 -> 57.1 us, 384 -> 1536 at 1576 8.9 -> 7.8.
-// The kinds from kKindActI8 on apply an activation and add a residual: more instructions and registers, and so kernels of their own.
-enum OutKind { kKindI8, kKindNext, kKindScatter, kKindHalf, kKindWord, kKindActI8, kKindActNext, kKindActScatter, kKindActHalf, kKindActWord };
-constexpr int kActKinds = kKindActI8 - kKindI8;
+// The kinds from kKindActI8 on apply an activation, those from kKindResI8 on add a residual too: more instructions and registers, and so kernels
+// of their own (768 -> 3072 at 12,608 rows, GELU, fp16: 41.6 us where one kernel may add a residual too, 32.7 in one that cannot).
+enum OutKind { kKindI8, kKindNext, kKindScatter, kKindHalf, kKindWord, kKindActI8, kKindActNext, kKindActScatter, kKindActHalf, kKindActWord,
+               kKindResI8, kKindResHalf, kKindResWord };
 static OutKind out_kind(int out_mode, bool staged)
 {
     return out_mode == FLEXIQ_OUT_REQUANT_I8 ? kKindI8 : out_mode == kOutNextSlab ? (staged ? kKindNext : kKindScatter)
@@ -292,52 +298,89 @@ __device__ __forceinline__ void next_slab16(const GemmParams &p, int ent, const 
         for (int q = 0; q < 4; ++q) out[q] &= mask;
     }
 }
-// Activation and residual: 16 accumulator columns of one row -> 16 fp32 values.  `res` = the row's residual at these columns, or NULL.
-__device__ __forceinline__ void add_residual16(int dtype, const void *res, float *v)
+// Activation and residual.  A lane's residual of 16 columns (32 or 64 bytes) in registers, as it is.
+struct ResidualUnit { uint32_t w[16]; };
+__device__ __forceinline__ void cp_async_16(uint32_t dst, const void *src)
 {
-    float x[16];
-    if (dtype == FLEXIQ_DTYPE_F32) load16<FLEXIQ_DTYPE_F32>(res, x);
-    else if (dtype == FLEXIQ_DTYPE_F16) load16<FLEXIQ_DTYPE_F16>(res, x);
-    else load16<FLEXIQ_DTYPE_BF16>(res, x);
+    asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+__device__ __forceinline__ void ld_shared_128(uint32_t src, uint32_t *w)
+{
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(src) : "memory");
+}
+__device__ __forceinline__ void add_residual16(int dtype, const ResidualUnit &u, pair_t *v)
+{
+    if (dtype == FLEXIQ_DTYPE_F32) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = __fadd_rn(v[i], x[i]);
+        for (int i = 0; i < 8; ++i) v[i] = add2(v[i], pair(__uint_as_float(u.w[2 * i]), __uint_as_float(u.w[2 * i + 1])));
+    } else if (dtype == FLEXIQ_DTYPE_F16) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&u.w[i]));
+            v[i] = add2(v[i], pair(f.x, f.y));
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = add2(v[i], pair(__uint_as_float(u.w[i] << 16), __uint_as_float(u.w[i] & 0xffff0000u)));
+    }
 }
-__device__ __forceinline__ void finish16_act(const GemmParams &p, const uint32_t *r, const float *alpha16, const float *beta16, const void *res, float *v)
+// 16 accumulator columns of one row -> 16 fp32 values
+template <bool RES>
+__device__ __forceinline__ void finish16_act(const GemmParams &p, const uint32_t *r, const float *alpha16, const float *beta16, const ResidualUnit &u, float *v)
 {
-    finish16<FLEXIQ_OUT_DEQUANT_F32>(r, alpha16, beta16, reinterpret_cast<uint32_t *>(v));
-    if (res && p.res_first) add_residual16(p.res_dtype, res, v);
-    activate_n<16>(p.act, v);
-    if (res && !p.res_first) add_residual16(p.res_dtype, res, v);
+    const ulonglong2 *fa = reinterpret_cast<const ulonglong2 *>(alpha16), *fb = reinterpret_cast<const ulonglong2 *>(beta16);
+    pair_t t[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const ulonglong2 a = fa[i], b = fb[i];
+        t[2 * i] = fma2(pair((float)(int)r[4 * i], (float)(int)r[4 * i + 1]), a.x, b.x);
+        t[2 * i + 1] = fma2(pair((float)(int)r[4 * i + 2], (float)(int)r[4 * i + 3]), a.y, b.y);
+    }
+    if (RES && p.res_first) add_residual16(p.res_dtype, u, t);
+    activate_n<8>(p.act, t);
+    if (RES && !p.res_first) add_residual16(p.res_dtype, u, t);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) unpair(t[i], &v[2 * i], &v[2 * i + 1]);
 }
-// Eq. 1 of 16 values, clipped to the integers lo and hi first: what the prologue makes of them
-__device__ __forceinline__ void quantize16_f32(const GemmParams &p, const float *v, float lo, float hi, uint32_t mask, uint32_t *out)
+// Eq. 1 of 16 values into int8, what the prologue makes of them.  The conversions saturate, so only the upper bound, which is also what a NaN
+// becomes, is set before them; `narrow`: clipped to [lo, hi] of fewer bits, the bits outside `mask` cleared.
+__device__ __forceinline__ void quantize16_f32(const GemmParams &p, const float *v, bool narrow, float lo, float hi, uint32_t mask, uint32_t *out)
 {
     float t[16];
     if (p.quot.form == kQuotTwoTerm) {
-        const TwoTerm div{p.quot.r_hi, p.quot.r_lo};
 #pragma unroll
-        for (int i = 0; i < 16; ++i) t[i] = TwoTerm::clip(div(v[i]), lo, hi);
+        for (int i = 0; i < 8; ++i) {
+            const pair_t x = pair(v[2 * i], v[2 * i + 1]);
+            unpair(fma2(x, pair(p.quot.r_hi, p.quot.r_hi), mul2(x, pair(p.quot.r_lo, p.quot.r_lo))), &t[2 * i], &t[2 * i + 1]);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) t[i] = fminf(t[i], hi);
     } else {
         const Divider div = make_divider(p.q_scale);
 #pragma unroll
         for (int i = 0; i < 16; ++i) t[i] = Divider::clip(div(v[i]), lo, hi);
     }
+    if (narrow) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) t[i] = fmaxf(t[i], lo);
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) out[i] = quant4(t[4 * i], t[4 * i + 1], t[4 * i + 2], t[4 * i + 3]) & mask;
 }
-// One 16-channel chunk of the fused layer boundary with an activation (`ent` as in next_slab16)
-__device__ __forceinline__ void next_slab16_act(const GemmParams &p, int ent, const uint32_t *r, const float *alpha16, const float *beta16, uint32_t *out)
+// The same for a 16-channel chunk of the next layer's slab (`ent` as in next_slab16)
+__device__ __forceinline__ void quantize16_next(const GemmParams &p, int ent, const float *v, uint32_t *out)
 {
-    float lo = -128.f, hi = 127.f, v[16];
+    float lo = -128.f, hi = 127.f;
     uint32_t mask = 0xffffffffu;
-    if ((ent & 0xffffff) * 16 < p.next_K_lo) {
+    const bool low = (ent & 0xffffff) * 16 < p.next_K_lo;
+    if (low) {
         const int sft = ent >> 24;
         hi = (float)(8 << sft) - 1.f;
         lo = -(float)(8 << sft);
         mask = ((0xffu << sft) & 0xffu) * 0x01010101u;
     }
-    finish16_act(p, r, alpha16, beta16, nullptr, v);
-    quantize16_f32(p, v, lo, hi, mask, out);
+    quantize16_f32(p, v, low, lo, hi, mask, out);
 }
 __device__ __forceinline__ void st_global_128(void *p, uint32_t a, uint32_t b, uint32_t c, uint32_t d)
 {
@@ -396,11 +439,20 @@ struct EpilogueCtx {
     uint64_t *tmem_full, *tmem_empty;
     volatile int *abort_flag;
     float *fac;
+    uint32_t res_stage;           // this warp's 2 KB for its residual
     uint32_t store_stage;         // this warp's 1 KB of shared memory for staged stores
     const CUtensorMap *map_y, *map_y16;   // boxes of 32 rows x 32 columns (32-byte swizzle) and 32 x 16 (plain)
     int first_tile, tile_step, num_tiles;
     int parts, arrivals_on;  // column parts per tile (4 or 2); this warp arrives on the accumulator barrier
 };
+
+// Row of Y of position k of a tile of the patch modes' grid; p.M or more: not an output pixel.
+__device__ __forceinline__ long long grid_row(const GemmParams &p, int mt, int ilog, int k)
+{
+    const int pw = 1 << p.pw_log2, img = mt / p.tiles_per_img;
+    const int yy = (mt - img * p.tiles_per_img) * p.TH + (k >> (p.pw_log2 + ilog)), xx = k & (pw - 1), nn = (img << ilog) + ((k >> p.pw_log2) & ((1 << ilog) - 1));
+    return (yy < p.P && xx < p.Q) ? ((long long)nn * p.P + yy) * p.Q + xx : p.M;
+}
 
 // One epilogue warp: TMEM lane quadrant `quad` (32 rows, lane = row), column slot `part` (32 or 64
 // columns per pass; two passes when only eight warps drain the tile) of every tile of this CTA.
@@ -409,7 +461,7 @@ struct EpilogueCtx {
 // 8 four-byte columns) and leave through tiled bulk stores.  The first half is stored before the accumulator goes back; against the one
 // kernel for all outputs, which read the whole slice first, no shape is slower for it (int8, GEMM alone: ViT-B QKV 19.2 -> 18.0 us,
 // fc2 22.3 -> 21.7, ViT-L fc2 70-83 and 70-86 us under the power cap).
-template <int CG, int MODE, bool SPLIT, int KIND, bool ACT = false>
+template <int CG, int MODE, bool SPLIT, int KIND, bool ACT = false, bool RES = false>
 __device__ __forceinline__ void epilogue_role(const GemmParams &p, const EpilogueCtx &x, int quad, int part, int lane)
 {
     constexpr bool kPatch = KIND == 2, kGrid = KIND >= 2;
@@ -431,10 +483,25 @@ __device__ __forceinline__ void epilogue_role(const GemmParams &p, const Epilogu
     PROF_DECL(prof_ld);
     PROF_DECL(prof_math);
     PROF_T0(prof_start);
-    // this lane's residual at output channel n (rows outside Y have none)
-    const int res_bytes = p.res_dtype == FLEXIQ_DTYPE_F32 ? 4 : 2;
-    auto residual = [&](long long r, int n) -> const void * {
-        return p.res && r < p.M ? static_cast<const char *>(p.res) + ((size_t)r * p.N + n) * res_bytes : nullptr;
+    // A residual comes through shared memory, 64 bytes of the warp's 32 rows at a time (16-bit: 32 columns, fp32: 16), by asynchronous
+    // copies of whole 64-byte pieces: the next piece, of the next tile where this one ends, is under way while one is worked on.  With each
+    // lane loading from its own row (32 bytes of 32 lines an instruction) the requests were the limit, whatever their width: 768 -> 3072 at
+    // 12,608 rows, fp16, 57.2 us (47 without allocation in L1), 43.7 so.  The 16-byte chunks of a row lie permuted, so that neither side
+    // meets a bank twice.  The ring gives up 22 KB for it: five stages of a 256-column pair's six, which costs nothing at 768 channels and up
+    // to 5 % at 3072 (four stages 15 %, hence no more than 64 bytes of a row at a time).
+    const int res_log = p.res_dtype == FLEXIQ_DTYPE_F32 ? 2 : 1;   // bytes of a value
+    bool res_asked = false;                      // the first piece of the coming pass is under way
+    auto request_residual = [&](long long r, int n) {
+        if (n >= p.N) return;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int rr = 8 * k + (lane >> 2), c = lane & 3;
+            const long long from = kGrid ? __shfl_sync(0xffffffffu, r, rr) : r - lane + rr;
+            // (the last piece of a row may be half a piece: N is a multiple of 16)
+            if (from < p.M && n + ((16 * c) >> res_log) < p.N)
+                cp_async_16(x.res_stage + (uint32_t)rr * 64u + (uint32_t)((c ^ ((rr >> 1) & 3)) << 4),
+                            static_cast<const char *>(p.res) + ((((size_t)from * p.N + n) << res_log) + 16 * c));
+        }
     };
     const int passes = 4 / x.parts;              // 1 with sixteen epilogue warps, 2 with eight
     // Patch mode keeps four accumulators, tile ti in accumulator ti mod 4.  With 64-column tiles only column
@@ -473,7 +540,7 @@ __device__ __forceinline__ void epilogue_role(const GemmParams &p, const Epilogu
             if (col0 >= BN) {
                 // no columns for this warp in this pass: only keep step with the accumulator barriers
                 if (!waited) {
-                    if (!__all_sync(0xffffffffu, wait_bounded(&x.tmem_full[buf], buf_phase, x.abort_flag, 4))) return;
+                    if (!__all_sync(0xffffffffu, wait_bounded(&x.tmem_full[buf], buf_phase, x.abort_flag, 4))) { if (RES) cp_async_wait(); return; }
                     waited = true;
                 }
                 if (pass + 1 == passes) {
@@ -487,13 +554,16 @@ __device__ __forceinline__ void epilogue_role(const GemmParams &p, const Epilogu
             }
             float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
             if (kScaled && nw + 4 * (lane & 15) < p.N) f = __ldg(reinterpret_cast<const float4 *>(fsrc + nw));
+            constexpr bool kScatterOut = MODE == kOutScatter;
+            if (RES && !res_asked) request_residual(row, nw);   // ahead of the wait for the accumulator
+            res_asked = false;
             int ent = 0;                                     // fused boundary: lane g fetches chunk g's slab entry
             if (kSlab && lane < 4 && nw + 16 * lane < p.N) ent = p.next_ent[(nw >> 4) + lane];
             if (!waited) {
                 PROF_T0(t0);
                 const bool ok = wait_bounded(&x.tmem_full[buf], buf_phase, x.abort_flag, 4);
                 PROF_ADD(prof_wait, t0);
-                if (!__all_sync(0xffffffffu, ok)) return;
+                if (!__all_sync(0xffffffffu, ok)) { if (RES) cp_async_wait(); return; }
                 ptx::tc_fence_after_sync();
                 waited = true;
             }
@@ -510,6 +580,137 @@ __device__ __forceinline__ void epilogue_role(const GemmParams &p, const Epilogu
                 for (int g = 0; g < 4; ++g) ents[g] = __shfl_sync(0xffffffffu, ent, g);
             }
             const long long row0 = kGrid ? (box_live ? 0 : p.M) : row - lane;
+            if constexpr (ACT) {
+                // 16 columns at a time
+                const int units = cols >> 4;
+                ResidualUnit res = {};
+                uint32_t chunk[8] = {};                            // scattered: the even unit's chunk, and the odd one's
+                int held_pos = 0;
+#pragma unroll 1
+                for (int u = 0; u < units; ++u) {
+                    const int n = nw + 16 * u;
+                    const bool live = n < p.N && row0 < p.M;   // warp-uniform
+                    uint32_t r[16];
+                    __syncwarp();                                  // rows beyond M rejoin
+                    ptx::tmem_ld_32x16(taddr + 16 * u, r);
+                    if (SPLIT) {                                   // the other MMA warp's partial sums (32-column passes only)
+                        uint32_t rb[16];
+                        ptx::tmem_ld_32x16(taddr + x.buf_stride + 16 * u, rb);
+                        ptx::tmem_ld_wait();
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) r[i] += rb[i];
+                    } else {
+                        ptx::tmem_ld_wait();
+                    }
+                    if (pass + 1 == passes && u + 1 == units) {
+                        ptx::tc_fence_before_sync();
+                        __syncwarp();
+                        if (lane == 0) {
+                            if (CG == 2) ptx::mbar_arrive_cluster_relaxed(ptx::mapa(ptx::smem_u32(&x.tmem_empty[buf]), 0));
+                            else ptx::mbar_arrive_relaxed(&x.tmem_empty[buf]);
+                        }
+                    }
+                    if (RES && n < p.N) {
+                        const int piece = 32 >> (res_log - 1);     // columns
+                        if (((16 * u) & (piece - 1)) == 0) {
+                            cp_async_wait();
+                            __syncwarp();
+#pragma unroll
+                            for (int c = 0; c < 4; ++c)
+                                ld_shared_128(x.res_stage + (uint32_t)lane * 64u + (uint32_t)((c ^ ((lane >> 1) & 3)) << 4), res.w + 4 * c);
+                            __syncwarp();                          // the piece is in registers: the next may come
+                            if (n + piece < p.N && 16 * u + piece < cols) request_residual(row, n + piece);
+                            else {
+                                const bool more = pass + 1 < passes;
+                                TileWalk to = tw;
+                                if (!more) to.next();
+                                if (more || to.left > 0) {
+                                    const int c0 = (part * passes + (more ? pass + 1 : 0)) * cols;
+                                    const long long r_to = kGrid ? grid_row(p, KIND == 3 ? to.m_blk * CG + (int)x.cta_rank : to.m_blk, KIND == 3 ? p.img_log2 : 0, quad * 32 + lane)
+                                                                 : ((long long)to.m_blk * CG + x.cta_rank) * BM + quad * 32 + lane;
+                                    if (c0 < BN && to.n_blk * BN + c0 < p.N) {
+                                        request_residual(r_to, to.n_blk * BN + c0);
+                                        res_asked = true;
+                                    }
+                                }
+                            }
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) res.w[i] = res.w[8 + i];   // 16-bit: the piece's second half
+                        }
+                    }
+                    if (!live) continue;
+                    float v[16];
+                    finish16_act<RES>(p, r, x.fac + 16 * u, x.fac + 64 + 16 * u, res, v);
+                    if (kScatterOut) {
+                        const int ent_u = u == 0 ? ents[0] : u == 1 ? ents[1] : u == 2 ? ents[2] : ents[3];
+                        quantize16_next(p, ent_u, v, chunk + 4);
+                        const int pos = ent_u & 0xffffff;
+                        if (row < p.M) {
+                            // chunks that lie side by side in the slab too go out as one whole sector
+                            const bool held = u & 1, hold = !held && n + 16 < p.N;
+                            uint8_t *srow = static_cast<uint8_t *>(p.Y) + row * p.N;
+                            if (held && pos == held_pos + 1 && (held_pos & 1) == 0 && ((reinterpret_cast<uintptr_t>(p.Y) | (uintptr_t)p.N) & 31) == 0)
+                                st_global_256(srow + held_pos * 16, chunk);
+                            else {
+                                if (held) st_global_128(srow + held_pos * 16, chunk[0], chunk[1], chunk[2], chunk[3]);
+                                if (!hold) st_global_128(srow + pos * 16, chunk[4], chunk[5], chunk[6], chunk[7]);
+                            }
+                        }
+                        held_pos = pos;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) chunk[i] = chunk[4 + i];
+                        continue;
+                    }
+                    const uint32_t dst = x.store_stage + (uint32_t)lane * 32u, sw16 = ((uint32_t)lane >> 2 & 1u) << 4;
+                    if (kElem == 1) {
+                        // a box of 32 columns takes two units; the last 16 channels of N a box of their own
+                        uint32_t w[4];
+                        if (MODE == kOutNextSlab) quantize16_next(p, u == 0 ? ents[0] : u == 1 ? ents[1] : u == 2 ? ents[2] : ents[3], v, w);
+                        else quantize16_f32(p, v, false, -128.f, 127.f, 0xffffffffu, w);
+                        const bool second = u & 1, both = second || n + 16 < p.N;
+                        if (!second) {
+                            if (lane == 0) ptx::bulk_wait_read_all();    // the previous store has read the buffer
+                            __syncwarp();
+                        }
+                        if (both) ptx::st_shared_128(dst + (second ? sw16 ^ 16u : sw16), w[0], w[1], w[2], w[3]);
+                        else ptx::st_shared_128(x.store_stage + (uint32_t)lane * 16u, w[0], w[1], w[2], w[3]);
+                        if (second || !both) {
+                            ptx::fence_proxy_async_smem();
+                            __syncwarp();
+                            if (lane == 0) {
+                                const CUtensorMap *map = both ? x.map_y : x.map_y16;
+                                const int col = second ? n - 16 : n;
+                                if (kGrid) store_box(map, col);
+                                else ptx::tma_store_2d(map, x.store_stage, col, (int)row0);
+                                ptx::bulk_commit_group();
+                            }
+                        }
+                        continue;
+                    }
+                    constexpr int kBoxes = kElem == 4 ? 2 : 1;     // 32-byte rows: 16 or 8 columns
+#pragma unroll
+                    for (int b = 0; b < kBoxes; ++b) {
+                        uint32_t w[8];
+#pragma unroll
+                        for (int q = 0; q < 8; ++q)
+                            w[q] = kHalf ? pack2_f16<MODE == FLEXIQ_OUT_DEQUANT_BF16>(v[2 * q], v[2 * q + 1]) : __float_as_uint(v[8 * b + q]);
+                        if (lane == 0) ptx::bulk_wait_read_all();
+                        __syncwarp();
+                        ptx::st_shared_128(dst + sw16, w[0], w[1], w[2], w[3]);
+                        ptx::st_shared_128(dst + (sw16 ^ 16u), w[4], w[5], w[6], w[7]);
+                        ptx::fence_proxy_async_smem();
+                        __syncwarp();
+                        if (lane == 0) {
+                            const int col = kElem * (n + 8 * b);   // in bytes
+                            if (kGrid) store_box(x.map_y, col);
+                            else ptx::tma_store_2d(x.map_y, x.store_stage, col, (int)row0);
+                            ptx::bulk_commit_group();
+                        }
+                    }
+                }
+                continue;
+            }
             // 32 columns at a time, in a loop: both halves' registers at once spilled, and the small launches pay for every
             // instruction that has to be fetched (the waits' slow path inlined: DeiT-S at batch 1 275 -> 284 us).
 #pragma unroll 1
@@ -550,18 +751,7 @@ __device__ __forceinline__ void epilogue_role(const GemmParams &p, const Epilogu
                             // is lowered when it lies below the next layer's max_4bit_ch
 #pragma unroll
                             for (int g = 0; g < 2; ++g)
-                                if (g == 0 || both) {
-                                    if (ACT) next_slab16_act(p, (h ? ents[2 + g] : ents[g]), r + 16 * g, fac + 16 * g, fac + 64 + 16 * g, w + 4 * g);
-                                    else next_slab16(p, (h ? ents[2 + g] : ents[g]), r + 16 * g, fac + 16 * g, fac + 64 + 16 * g, w + 4 * g);
-                                }
-                        } else if (ACT) {
-#pragma unroll
-                            for (int g = 0; g < 2; ++g)
-                                if (g == 0 || both) {
-                                    float v[16];
-                                    finish16_act(p, r + 16 * g, fac + 16 * g, fac + 64 + 16 * g, residual(row, n + 16 * g), v);
-                                    quantize16_f32(p, v, -128.f, 127.f, 0xffffffffu, w + 4 * g);
-                                }
+                                if (g == 0 || both) next_slab16(p, (h ? ents[2 + g] : ents[g]), r + 16 * g, fac + 16 * g, fac + 64 + 16 * g, w + 4 * g);
                         } else {
                             finish16<FLEXIQ_OUT_REQUANT_I8>(r, fac, fac + 64, w);
                             if (both) finish16<FLEXIQ_OUT_REQUANT_I8>(r + 16, fac + 16, fac + 64 + 16, w + 4);
@@ -591,8 +781,7 @@ __device__ __forceinline__ void epilogue_role(const GemmParams &p, const Epilogu
                         const int n = nw + 32 * h + 16 * g;
                         if (n < p.N && row0 < p.M) {   // warp-uniform
                             uint32_t w[16], hw[8];
-                            if (ACT) finish16_act(p, r + 16 * g, fac + 16 * g, fac + 64 + 16 * g, residual(row, n), reinterpret_cast<float *>(w));
-                            else finish16<FLEXIQ_OUT_DEQUANT_F32>(r + 16 * g, fac + 16 * g, fac + 64 + 16 * g, w);
+                            finish16<FLEXIQ_OUT_DEQUANT_F32>(r + 16 * g, fac + 16 * g, fac + 64 + 16 * g, w);
 #pragma unroll
                             for (int q = 0; q < 8; ++q)
                                 hw[q] = pack2_f16<MODE == FLEXIQ_OUT_DEQUANT_BF16>(__uint_as_float(w[2 * q]), __uint_as_float(w[2 * q + 1]));
@@ -618,8 +807,7 @@ __device__ __forceinline__ void epilogue_role(const GemmParams &p, const Epilogu
                         const int n = nw + 32 * h + 16 * g;
                         if (n < p.N && row0 < p.M) {   // warp-uniform
                             uint32_t w[16];
-                            if (ACT) finish16_act(p, r + 16 * g, fac + 16 * g, fac + 64 + 16 * g, residual(row, n), reinterpret_cast<float *>(w));
-                            else finish16<MODE>(r + 16 * g, fac + 16 * g, fac + 64 + 16 * g, w);
+                            finish16<MODE>(r + 16 * g, fac + 16 * g, fac + 64 + 16 * g, w);
                             const uint32_t dst = x.store_stage + (uint32_t)lane * 32u;
                             const uint32_t sw16 = ((uint32_t)lane >> 2 & 1u) << 4;
 #pragma unroll
@@ -652,8 +840,7 @@ __device__ __forceinline__ void epilogue_role(const GemmParams &p, const Epilogu
                         for (int g = 0; g < 2; ++g) {
                             if (g == 0 || second) {
                                 pos[g] = (h ? ents[2 + g] : ents[g]) & 0xffffff;
-                                if (ACT) next_slab16_act(p, (h ? ents[2 + g] : ents[g]), r + 16 * g, fac + 16 * g, fac + 64 + 16 * g, w + 4 * g);
-                                else next_slab16(p, (h ? ents[2 + g] : ents[g]), r + 16 * g, fac + 16 * g, fac + 64 + 16 * g, w + 4 * g);
+                                next_slab16(p, (h ? ents[2 + g] : ents[g]), r + 16 * g, fac + 16 * g, fac + 64 + 16 * g, w + 4 * g);
                             }
                         }
                         if (second && wide && pos[1] == pos[0] + 1 && (pos[0] & 1) == 0) st_global_256(srow + pos[0] * 16, w);
@@ -701,7 +888,7 @@ mixed_gemm_kernel(const __grid_constant__ CUtensorMap mapA_lo, const __grid_cons
         return;
     }
     uint8_t *stage_base = smem;
-    uint8_t *factors = smem + kStageRegion;
+    uint8_t *factors = smem + (OUT >= kKindResI8 ? kStageRegionRes : kStageRegion);
     uint8_t *store_stage = factors + kNumWorkWarps * kFactorsPerWarp;  // 1024-byte aligned: the bulk stores' swizzle needs it
     uint64_t *full_bar = reinterpret_cast<uint64_t *>(store_stage + kNumWorkWarps * kStoreStagePerWarp);
     uint64_t *empty_bar = full_bar + kMaxStages;
@@ -1313,19 +1500,19 @@ mixed_gemm_kernel(const __grid_constant__ CUtensorMap mapA_lo, const __grid_cons
             x.tmem_full = tmem_full; x.tmem_empty = tmem_empty; x.abort_flag = abort_flag;
             x.fac = reinterpret_cast<float *>(factors + e * kFactorsPerWarp);  // alpha[64] | beta[64]
             x.store_stage = ptx::smem_u32(store_stage + e * kStoreStagePerWarp);
+            x.res_stage = ptx::smem_u32(store_stage + kNumWorkWarps * kStoreStagePerWarp + 256 + e * kResPerWarp);
             x.map_y = &mapY; x.map_y16 = &mapY16;
             x.first_tile = first_tile; x.tile_step = tile_step; x.num_tiles = num_tiles;
             x.parts = kEpiWarps / 4; x.arrivals_on = 1;
-            constexpr bool kAct = OUT >= kActKinds;
-            constexpr int kOut = kAct ? OUT - kActKinds : OUT;
-            if constexpr (kOut == kKindI8) epilogue_role<CG, FLEXIQ_OUT_REQUANT_I8, SPLIT, KIND, kAct>(p, x, warp & 3, e >> 2, lane);
-            else if constexpr (kOut == kKindNext) epilogue_role<CG, kOutNextSlab, SPLIT, KIND, kAct>(p, x, warp & 3, e >> 2, lane);
-            else if constexpr (kOut == kKindScatter) epilogue_role<CG, kOutScatter, SPLIT, KIND, kAct>(p, x, warp & 3, e >> 2, lane);
-            else if constexpr (kOut == kKindHalf) {
-                if (p.out_mode == FLEXIQ_OUT_DEQUANT_F16) epilogue_role<CG, FLEXIQ_OUT_DEQUANT_F16, SPLIT, KIND, kAct>(p, x, warp & 3, e >> 2, lane);
-                else epilogue_role<CG, FLEXIQ_OUT_DEQUANT_BF16, SPLIT, KIND, kAct>(p, x, warp & 3, e >> 2, lane);
+            constexpr bool kAct = OUT >= kKindActI8, kRes = OUT >= kKindResI8;
+            if constexpr (OUT == kKindI8 || OUT == kKindActI8 || OUT == kKindResI8) epilogue_role<CG, FLEXIQ_OUT_REQUANT_I8, SPLIT, KIND, kAct, kRes>(p, x, warp & 3, e >> 2, lane);
+            else if constexpr (OUT == kKindNext || OUT == kKindActNext) epilogue_role<CG, kOutNextSlab, SPLIT, KIND, kAct>(p, x, warp & 3, e >> 2, lane);
+            else if constexpr (OUT == kKindScatter || OUT == kKindActScatter) epilogue_role<CG, kOutScatter, SPLIT, KIND, kAct>(p, x, warp & 3, e >> 2, lane);
+            else if constexpr (OUT == kKindHalf || OUT == kKindActHalf || OUT == kKindResHalf) {
+                if (p.out_mode == FLEXIQ_OUT_DEQUANT_F16) epilogue_role<CG, FLEXIQ_OUT_DEQUANT_F16, SPLIT, KIND, kAct, kRes>(p, x, warp & 3, e >> 2, lane);
+                else epilogue_role<CG, FLEXIQ_OUT_DEQUANT_BF16, SPLIT, KIND, kAct, kRes>(p, x, warp & 3, e >> 2, lane);
             } else {
-                if (kAct || p.out_mode == FLEXIQ_OUT_DEQUANT_F32) epilogue_role<CG, FLEXIQ_OUT_DEQUANT_F32, SPLIT, KIND, kAct>(p, x, warp & 3, e >> 2, lane);
+                if (kAct || p.out_mode == FLEXIQ_OUT_DEQUANT_F32) epilogue_role<CG, FLEXIQ_OUT_DEQUANT_F32, SPLIT, KIND, kAct, kRes>(p, x, warp & 3, e >> 2, lane);
                 else epilogue_role<CG, FLEXIQ_OUT_ACC_I32, SPLIT, KIND>(p, x, warp & 3, e >> 2, lane);
             }
         } else if (PK && warp < 2 + kNumWorkWarps) {
@@ -1616,7 +1803,7 @@ static int make_map_nhwc_by_row(CUtensorMap *map, const void *base, uint64_t row
 }
 
 // What decides between the kinds a convolution can run as.
-struct ConvShape { int C, N, R, S, stride, pad, Nb, W, P, Q, bk; };
+struct ConvShape { int C, N, R, S, stride, pad, Nb, W, P, Q, bk, region; };   // region: bytes of the rings
 
 // Patch mode (see GemmParams): stride-1 filters of more than one tap whose channels fit one K block and whose
 // output channels fit one tile, the weights of all taps resident in shared memory.
@@ -1632,7 +1819,7 @@ static bool plan_patch(const ConvShape &c, PatchPlan *out)
     p.rows = p.th + c.R - 1 + (c.W + 2 * c.pad > (1 << p.pw_log2) ? 1 : 0);
     p.stage = (((p.rows << p.pw_log2) * c.bk) + 1023) & ~1023;
     const int b_all = ((c.R * c.S * p.bn * c.bk) + 1023) & ~1023;
-    if (b_all + 2 * p.stage > kStageRegion || p.rows > 256) return false;
+    if (b_all + 2 * p.stage > c.region || p.rows > 256) return false;
     p.tiles_per_img = (c.P + p.th - 1) / p.th;
     *out = p;
     return true;
@@ -1688,7 +1875,7 @@ static bool plan_stream(const ConvShape &c, TileChoice im2col, int sms, StreamPl
     const int nbt = (c.C + c.bk - 1) / c.bk;
     for (int cg = 2; cg >= 1; --cg)
         for (int bn = 128; bn >= 64; bn -= 64) {
-            const int st = (kStageRegion - 2 * s.a_stage) / (c.S * (bn / cg) * c.bk);
+            const int st = (c.region - 2 * s.a_stage) / (c.S * (bn / cg) * c.bk);
             if (st < 2) continue;
             const long long tiles = (s.m_tiles + cg - 1) / cg * ((c.N + bn - 1) / bn), waves = (tiles + sms / cg - 1) / (sms / cg);
             const double cost = (double)waves * ((double)nbt * c.R * c.S * (c.bk / 32) * per_step(cg, bn) + 1200.0) + (cg == 2 ? 800.0 : 0.0);
@@ -1718,7 +1905,7 @@ static int launch_kernel(const LaunchMaps &m, const GemmParams &p, int sms, cuda
     int dev = 0;
     cudaGetDevice(&dev);
     if (dev >= 64 || !attr_set[dev]) {
-        FLEXIQ_CUDA_TRY(cudaFuncSetAttribute(mixed_gemm_kernel<CG, PK, KIND, SPLIT, OUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes));
+        FLEXIQ_CUDA_TRY(cudaFuncSetAttribute(mixed_gemm_kernel<CG, PK, KIND, SPLIT, OUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, OUT >= kKindResI8 ? kSmemBytesRes : kSmemBytes));
         if (dev < 64) attr_set[dev] = true;
     }
     const long long tiles = (long long)p.m_tiles * p.n_tiles;
@@ -1727,7 +1914,7 @@ static int launch_kernel(const LaunchMaps &m, const GemmParams &p, int sms, cuda
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(grid, 1, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
-    cfg.dynamicSmemBytes = kSmemBytes;
+    cfg.dynamicSmemBytes = OUT >= kKindResI8 ? kSmemBytesRes : kSmemBytes;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -1835,6 +2022,7 @@ static int run_mixed(Layer *L, const uint8_t *X4, const int8_t *X8, const uint8_
     } else if ((rc = check_slab(L, X4, "X4_dev"))) return rc;
     const int sms = device_sm_count(L->device);
 
+    const int region = ops && ops->res ? kStageRegionRes : kStageRegion;
     GemmParams p{};
     p.M = M; p.N = L->N; p.C = L->C; p.C_lo = packed ? C_lo : 0; p.C_hi = packed ? C_hi : L->C;
     p.T = L->R * L->S; p.S = L->S;
@@ -1938,7 +2126,7 @@ static int run_mixed(Layer *L, const uint8_t *X4, const int8_t *X8, const uint8_
     bool patch = false, stream = false;
     StreamPlan sp{};
     if (!packed && !g_forced_tile.cg && p.im2col) {
-        const ConvShape shape{L->C, L->N, L->R, L->S, L->stride, L->pad, Nb, W, p.P, p.Q, p.BK};
+        const ConvShape shape{L->C, L->N, L->R, L->S, L->stride, L->pad, Nb, W, p.P, p.Q, p.BK, region};
         PatchPlan pp{};
         if ((patch = plan_patch(shape, &pp))) {
             tc.cg = 1; tc.bn = pp.bn;
@@ -1966,21 +2154,21 @@ static int run_mixed(Layer *L, const uint8_t *X4, const int8_t *X8, const uint8_
         p.tps = L->S < limit ? L->S : limit;
         if (p.tps < 1) p.tps = 1;
     }
-    p.stages = kStageRegion / (p.tps * (BM + bn / cg) * p.BK);
+    p.stages = region / (p.tps * (BM + bn / cg) * p.BK);
     if (!stream && p.tps > 1 && p.n_tiles == 1) {
         const int b_all = ((p.T * (bn / cg) * p.BK + 1023) / 1024) * 1024;
-        const int st = (kStageRegion - b_all) / (p.tps * BM * p.BK);
+        const int st = (region - b_all) / (p.tps * BM * p.BK);
         if (b_all <= 65536 && st >= 4) { p.b_res = 1; p.stages = st; }
     }
     if (patch) {
         p.b_res = 1;
-        p.stages = (kStageRegion - (((p.T * bn * p.BK) + 1023) & ~1023)) / p.patch_stage;
+        p.stages = (region - (((p.T * bn * p.BK) + 1023) & ~1023)) / p.patch_stage;
     }
     if (stream) p.stages = sp.stages;
     if (p.stages > kMaxStages) p.stages = kMaxStages;
     if (packed) {  // room for the ring of raw 4-bit tiles behind the operand ring
         const int raw = kRawStages * (BM + bn) * (p.BK / 2);
-        p.stages = (kStageRegion - raw) / ((BM + bn) * p.BK);
+        p.stages = (region - raw) / ((BM + bn) * p.BK);
         if (p.stages > kMaxStages) p.stages = kMaxStages;
     }
     // activation maps (per call: they depend on the caller's buffers, M and the ratio);
@@ -2080,14 +2268,20 @@ static int run_mixed(Layer *L, const uint8_t *X4, const int8_t *X8, const uint8_
     LaunchMaps maps{a_lo, a_hi, packed ? L->map_w4[bi] : L->map_w8m[bi], L->map_w8[bi], packed ? L->map_w8[bi] : L->map_wst[bi], y_map, y_map16};
     if (one_block && b_whole != 0) maps.b_hi = b_whole == 1 ? L->map_w8m[bi] : L->map_wst[bi];
     const LaunchForm form{cg, packed, patch, stream, conv_kind, split};
-    if (ops) switch (out_kind(out_mode, staged)) {
+    const OutKind kind = out_kind(out_mode, staged);
+    if (ops && ops->res) switch (kind) {
+        case kKindI8: rc = launch_form<kKindResI8>(form, maps, p, sms, st); break;
+        case kKindHalf: rc = launch_form<kKindResHalf>(form, maps, p, sms, st); break;
+        default: rc = launch_form<kKindResWord>(form, maps, p, sms, st); break;
+    }
+    else if (ops) switch (kind) {
         case kKindI8: rc = launch_form<kKindActI8>(form, maps, p, sms, st); break;
         case kKindScatter: rc = launch_form<kKindActScatter>(form, maps, p, sms, st); break;
         case kKindNext: rc = launch_form<kKindActNext>(form, maps, p, sms, st); break;
         case kKindHalf: rc = launch_form<kKindActHalf>(form, maps, p, sms, st); break;
         default: rc = launch_form<kKindActWord>(form, maps, p, sms, st); break;
     }
-    else switch (out_kind(out_mode, staged)) {
+    else switch (kind) {
         case kKindI8: rc = launch_form<kKindI8>(form, maps, p, sms, st); break;
         case kKindScatter: rc = launch_form<kKindScatter>(form, maps, p, sms, st); break;
         case kKindNext: rc = launch_form<kKindNext>(form, maps, p, sms, st); break;
@@ -2249,7 +2443,7 @@ extern "C" int flexiq_choose_conv_kind(int Nb, int H, int W, int Cin, int Cout, 
         H + 2 * pad < R || W + 2 * pad < S)
         return set_error(FLEXIQ_ERR_INVALID_ARG, "flexiq_choose_conv_kind: sizes must be positive, the filter must fit the padded input, output non-NULL");
     const int P = (H + 2 * pad - R) / stride + 1, Q = (W + 2 * pad - S) / stride + 1, bk = Cin >= 128 ? 128 : 64;
-    const ConvShape shape{Cin, Cout, R, S, stride, pad, Nb, W, P, Q, bk};
+    const ConvShape shape{Cin, Cout, R, S, stride, pad, Nb, W, P, Q, bk, kStageRegion};
     PatchPlan pp{};
     StreamPlan sp{};
     if (R == 1 && S == 1 && stride == 1 && pad == 0) *kind_out = 0;

@@ -114,9 +114,7 @@ __global__ void __launch_bounds__(kNormThreads) group_norm_kernel(const NormArgs
             const size_t row = row0 + i / cpg;
             const float d = load_as_f32(a.X, row * a.C + c, a.x_dtype) - mean;
             const float scale = rstd * (a.gamma ? a.gamma[c] : 1.f);
-            float y = fmaf(d, scale, fmaf(-off, scale, a.beta ? a.beta[c] : 0.f));
-            activate_n<1>(a.act, &y);
-            store_one(a.out, row, a.C, c, y);
+            store_one(a.out, row, a.C, c, activate_one(a.act, fmaf(d, scale, fmaf(-off, scale, a.beta ? a.beta[c] : 0.f))));
         }
     }
 }
