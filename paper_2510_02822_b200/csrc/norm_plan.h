@@ -1,0 +1,88 @@
+// How a group normalisation is cut up for its shape (host only; flexiq_norm.cu has the kernels).
+#pragma once
+#include "flexiq.h"
+
+namespace flexiq {
+
+constexpr int kNormThreads = 256;
+constexpr int kNormCluster = 8;        // blocks of a cluster at most ("held")
+constexpr int kNormSplits = 64;        // pieces of an image's channel block at most ("twice")
+constexpr int kMaxGroups = 128;        // groups of a channel block at most
+
+enum NormKind { kNormRows, kNormHeld, kNormTwice };
+struct NormPlan { NormKind kind; int vec, nv, threads, gpb, nch, cpt, lanes, cluster; long long span; bool many; };
+
+inline int gcd(int a, int b) { while (b) { const int t = a % b; a = b; b = t; } return a; }
+inline long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
+inline int round_up_pow2(long long v) { int p = 1; while (p < v) p <<= 1; return p; }
+
+// (a function of the shape alone, so that the scratch size can be asked for)
+inline NormPlan plan_norm(int x_dtype, long long Nb, long long P, int C, int groups, int sms)
+{
+    const int bytes = x_dtype == FLEXIQ_DTYPE_F32 ? 4 : 2, full = 16 / bytes, cpg = C / groups;
+    NormPlan p{};
+    p.cpt = 1;
+    if (P == 1) {
+        const int vec = cpg % full == 0 ? full : 1, nv = (int)ceil_div(cpg / vec, 32);
+        if (nv <= 8) {
+            p.kind = kNormRows; p.vec = vec; p.nv = nv; p.nch = cpg / vec;
+            return p;
+        }
+    }
+    // the smallest block of whole groups and whole pieces, then more groups until a position's part is 128 bytes
+    const int base_groups = C % full == 0 ? full / gcd(cpg, full) : 1;
+    const long long base_pieces = (long long)base_groups * cpg / full;
+    p.vec = C % full == 0 && (base_pieces <= kNormThreads || cpg % full == 0) ? full : 1;
+    const int unit_groups = p.vec == 1 ? 1 : base_groups, units = groups / unit_groups;
+    auto shape = [&](int m) {   // m of the smallest blocks together
+        p.gpb = unit_groups * m;
+        p.nch = (int)((long long)p.gpb * cpg / p.vec);
+        p.many = p.vec > 1 && cpg % p.vec != 0;
+        p.cpt = (int)ceil_div(p.nch, kNormThreads);
+    };
+    int m = 1;
+    while (m < units && (long long)unit_groups * m * cpg * bytes < 128 && unit_groups * m < kMaxGroups / 2) {
+        int next = m + 1;
+        while (units % next) ++next;
+        if ((long long)unit_groups * next * cpg / p.vec > kNormThreads || unit_groups * next > kMaxGroups) break;
+        m = next;
+    }
+    constexpr int kMaxNv = 16;
+    for (int w = m; w >= 1; --w) {
+        if (units % w) continue;
+        shape(w);
+        const long long capacity = p.cpt > 1 ? kMaxNv / p.cpt : (long long)(kNormThreads / p.nch) * kMaxNv;   // positions a block holds
+        if (capacity < 1 || ceil_div(P, capacity) > kNormCluster) continue;
+        p.kind = kNormHeld;
+        p.threads = kNormThreads;
+        const long long blocks = Nb * (units / w);
+        int k = round_up_pow2(ceil_div(P, capacity));
+        // more blocks where the machine has room for them and a thread more than one piece
+        while (k < kNormCluster && blocks * k * 2 <= 2 * sms && ceil_div(P, k) > (p.cpt > 1 ? 1 : kNormThreads / p.nch)) k *= 2;
+        p.cluster = k;
+        p.span = ceil_div(P, k);
+        if (p.cpt == 1) {
+            while (p.threads > 64 && p.threads / 2 >= p.nch && ceil_div(p.span, p.threads / 2 / p.nch) <= 4) p.threads /= 2;
+            p.lanes = p.threads / p.nch;
+            p.nv = round_up_pow2(ceil_div(p.span, p.lanes));
+        } else {
+            p.lanes = 1;
+            p.nv = round_up_pow2(p.span * p.cpt);
+        }
+        return p;
+    }
+    shape(m);
+    p.kind = kNormTwice;
+    p.threads = kNormThreads;
+    p.lanes = p.cpt > 1 ? 1 : kNormThreads / p.nch;
+    // pieces: some four blocks an SM, and at least a few steps each
+    const long long blocks = Nb * (units / m), steps = p.cpt > 1 ? P : ceil_div(P, (long long)p.lanes * 8);
+    long long k = ceil_div(4ll * sms, blocks);
+    if (k > steps) k = steps;
+    if (k > kNormSplits) k = kNormSplits;
+    p.cluster = (int)(k < 1 ? 1 : k);
+    p.span = ceil_div(P, p.cluster);
+    return p;
+}
+
+}  // namespace flexiq

@@ -352,6 +352,9 @@ __device__ __forceinline__ void cluster_sync_all()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// The same in two halves: what lies between them may not touch the other CTAs' memory.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 // TMA loads of a CTA pair: data lands in the executing CTA, the transaction bytes are
 // credited to the mbarrier at `mbar_cluster_addr` (the leader CTA's).  No multicast.
 __device__ __forceinline__ void tma_load_2d_pair(void *dst, const CUtensorMap *m, uint32_t mbar_cluster_addr, int x, int y)

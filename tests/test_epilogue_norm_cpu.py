@@ -46,7 +46,8 @@ def test_group_norm_nothing_to_do(lib):
 
 
 def test_scratch_size(lib):
-    assert fx.flexiq_group_norm_scratch(fx.DTYPE_F16, 1, 49, 512, 32) == 0
+    assert fx.flexiq_group_norm_scratch(fx.DTYPE_F16, 1, 49, 512, 32) == 0 and fx.flexiq_group_norm_scratch(fx.DTYPE_F16, 0, 1 << 20, 64, 32) == 0
+    assert fx.flexiq_group_norm_scratch(fx.DTYPE_F16, 3, 1 << 20, 64, 32) >= 3 * 32 * 8
     for bad in [(3, 1, 1, 32, 4), (0, -1, 1, 32, 4), (0, 1, 1, 32, 5), (0, 1, 1, 0, 1)]:
         with pytest.raises(fx.FlexiqError):
             fx.flexiq_group_norm_scratch(*bad)
