@@ -107,7 +107,8 @@ template <int ACT> __device__ __forceinline__ void activate2(float &a, float &b)
         const pair_t e = pair(exp2_approx(za), exp2_approx(zb));
         unpair(add2(e, pair(1.f, 1.f)), &da, &db);
         const float r = rcp_approx(__fmul_rn(da, db));
-        unpair(fma2(mul2(x, e), mul2(pair(r, r), pair(db, da)), pair(ma, mb)), &a, &b);
+        // (products one by one: a pair in another order, or of one value twice, has to be moved together first)
+        unpair(fma2(mul2(x, e), pair(__fmul_rn(r, db), __fmul_rn(r, da)), pair(ma, mb)), &a, &b);
     } else {
         typedef LogTail<ACT> F;
         const pair_t x = pair(fmaxf(-fabsf(a), -F::bound), fmaxf(-fabsf(b), -F::bound));

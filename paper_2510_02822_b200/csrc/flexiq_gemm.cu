@@ -300,11 +300,6 @@ __device__ __forceinline__ void next_slab16(const GemmParams &p, int ent, const 
 }
 // Activation and residual.  A lane's residual of 16 columns (32 or 64 bytes) in registers, as it is.
 struct ResidualUnit { uint32_t w[16]; };
-__device__ __forceinline__ void cp_async_16(uint32_t dst, const void *src)
-{
-    asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 __device__ __forceinline__ void ld_shared_128(uint32_t src, uint32_t *w)
 {
     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(src) : "memory");
@@ -499,7 +494,7 @@ __device__ __forceinline__ void epilogue_role(const GemmParams &p, const Epilogu
             const long long from = kGrid ? __shfl_sync(0xffffffffu, r, rr) : r - lane + rr;
             // (the last piece of a row may be half a piece: N is a multiple of 16)
             if (from < p.M && n + ((16 * c) >> res_log) < p.N)
-                cp_async_16(x.res_stage + (uint32_t)rr * 64u + (uint32_t)((c ^ ((rr >> 1) & 3)) << 4),
+                ptx::cp_async_16(x.res_stage + (uint32_t)rr * 64u + (uint32_t)((c ^ ((rr >> 1) & 3)) << 4),
                             static_cast<const char *>(p.res) + ((((size_t)from * p.N + n) << res_log) + 16 * c));
         }
     };
@@ -540,7 +535,7 @@ __device__ __forceinline__ void epilogue_role(const GemmParams &p, const Epilogu
             if (col0 >= BN) {
                 // no columns for this warp in this pass: only keep step with the accumulator barriers
                 if (!waited) {
-                    if (!__all_sync(0xffffffffu, wait_bounded(&x.tmem_full[buf], buf_phase, x.abort_flag, 4))) { if (RES) cp_async_wait(); return; }
+                    if (!__all_sync(0xffffffffu, wait_bounded(&x.tmem_full[buf], buf_phase, x.abort_flag, 4))) { if (RES) ptx::cp_async_wait(); return; }
                     waited = true;
                 }
                 if (pass + 1 == passes) {
@@ -563,7 +558,7 @@ __device__ __forceinline__ void epilogue_role(const GemmParams &p, const Epilogu
                 PROF_T0(t0);
                 const bool ok = wait_bounded(&x.tmem_full[buf], buf_phase, x.abort_flag, 4);
                 PROF_ADD(prof_wait, t0);
-                if (!__all_sync(0xffffffffu, ok)) { if (RES) cp_async_wait(); return; }
+                if (!__all_sync(0xffffffffu, ok)) { if (RES) ptx::cp_async_wait(); return; }
                 ptx::tc_fence_after_sync();
                 waited = true;
             }
@@ -613,7 +608,7 @@ __device__ __forceinline__ void epilogue_role(const GemmParams &p, const Epilogu
                     if (RES && n < p.N) {
                         const int piece = 32 >> (res_log - 1);     // columns
                         if (((16 * u) & (piece - 1)) == 0) {
-                            cp_async_wait();
+                            ptx::cp_async_wait();
                             __syncwarp();
 #pragma unroll
                             for (int c = 0; c < 4; ++c)
@@ -2480,7 +2475,9 @@ extern "C" int flexiq_check_status(void *stream)
     FLEXIQ_CUDA_TRY(cudaMemcpyFromSymbol(&word, g_status_word, sizeof(word)));
     if (word != 0) FLEXIQ_CUDA_TRY(cudaMemcpyToSymbol(g_status_word, &zero, sizeof(zero)));
     const unsigned int prologue_word = prologue_status();
+    const unsigned int norm_word = norm_status();
     if (word == 0) word = prologue_word;
+    if (word == 0) word = norm_word;
     if (word != 0) return set_error(FLEXIQ_ERR_TIMEOUT, "a bounded device-side wait expired (status word 0x%x)", word);
     return FLEXIQ_OK;
 }

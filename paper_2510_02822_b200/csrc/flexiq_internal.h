@@ -144,6 +144,7 @@ int make_map_2d(CUtensorMap *map, const void *base, uint64_t row_bytes, uint64_t
 
 // status word of the prologue's bounded waits (0 = none expired), cleared when read
 unsigned prologue_status();
+unsigned norm_status();   // the same of the group normalisation's
 
 int choose_bk(const Layer *L);
 int encode_weight_maps(Layer *L);

@@ -4,7 +4,7 @@
 //
 // Bound by memory: every input byte is to be read once and every output byte written once.  Three ways, by what fits where:
 //   rows   one position per image (layer normalisation): a warp holds a group in registers
-//   held   an image's block of channels (whole groups, 128 bytes a position where that is enough) is held in the registers of a block, or of a
+//   held   an image's block of channels (whole groups, 128 bytes a position where that is enough) is held in the shared memory of a block, or of a
 //          cluster of up to eight, between the statistics and their use; the blocks of a cluster exchange their groups' statistics
 //          through distributed shared memory
 //   twice  larger images: the statistics of pieces of an image go to scratch memory, and a second kernel reads the input again, in
@@ -13,8 +13,9 @@
 // Statistics.  The variance is a mean square of deviations, never a difference of two sums, which would lose everything where the mean
 // is large against the deviation.  A thread takes the mean and the sum of squared deviations M2 of its own values (at most 128, in registers, two
 // passes); those are joined in a fixed order by
-//   mean = ref + sum n_i (mean_i - ref) / n,   M2 = sum M2_i + n_i (mean_i - mean)^2          (ref: one of the means)
-// over the threads, the cluster's blocks or the pieces.  No sum is longer than some sixty roundings, and results do not depend on timing.
+//   m = sum n_i mean_i / n,   q_i = mean_i - m,   mean = m + sum n_i q_i / n,   M2 = sum M2_i + n_i q_i^2
+// over the threads, the cluster's blocks or the pieces.  (The second sum takes out what the first has rounded.  The first is not taken from one of
+// the means: where that one holds an outlier, its rounding would be the error.)  No sum is longer than some sixty roundings, and results do not depend on timing.
 #include "flexiq_internal.h"
 
 #include <cuda_bf16.h>
@@ -52,38 +53,45 @@ struct NormArgs {
     int cpt;                  // pieces of a position a thread has where there are more than threads, else 1
     int lanes;                // positions side by side in a block
     int cluster;              // blocks per image and channel block ("held"), or pieces of the image ("twice")
+    int cluster_log;          // "held": its logarithm
     long long span;           // positions of one of them
+    unsigned by_nch, by_lanes, by_cpg, by_each;   // 2^32 / those, rounded up: quotients of less than 2^16 by a multiplication
     float2 *stats;            // "twice": [image][group][piece] mean, M2
 };
 
-__device__ __forceinline__ uint4 load_piece(const void *p)
-{
-    uint4 u;
-    asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "l"(p) : "memory");
-    return u;
-}
-
-// VEC values in a row as they are: a 16-byte piece, or one value
+// VEC values in a row as they are: a 16-byte piece, or one value widened
 template <int DT, int VEC> struct Piece {
-    static constexpr int kBytes = DT == FLEXIQ_DTYPE_F32 ? 4 : 2;
-    typename std::conditional<VEC == 1, float, uint4>::type raw;
-    __device__ __forceinline__ void load(const void *X, size_t i)
+    static constexpr int kBytes = DT == FLEXIQ_DTYPE_F32 ? 4 : 2, kPairs = VEC == 1 ? 1 : VEC / 2;
+    typedef typename std::conditional<VEC == 1, float, uint4>::type Raw;
+    Raw raw;
+    __device__ __forceinline__ void load(const char *p)
     {
-        const char *p = static_cast<const char *>(X) + i * kBytes;
         if constexpr (VEC == 1) {
             if (DT == FLEXIQ_DTYPE_F32) raw = *reinterpret_cast<const float *>(p);
             else if (DT == FLEXIQ_DTYPE_F16) raw = __half2float(*reinterpret_cast<const __half *>(p));
             else raw = __bfloat162float(*reinterpret_cast<const __nv_bfloat16 *>(p));
         } else {
-            raw = load_piece(p);
+            asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(raw.x), "=r"(raw.y), "=r"(raw.z), "=r"(raw.w) : "l"(p) : "memory");
         }
     }
-    __device__ __forceinline__ void widen(float *x) const
+    // in pairs of fp32 (a single value: with a zero beside it)
+    __device__ __forceinline__ void widen(pair_t *x) const
     {
-        if constexpr (VEC == 1) x[0] = raw;
-        else {
+        if constexpr (VEC == 1) x[0] = pair(raw, 0.f);
+        else if constexpr (DT == FLEXIQ_DTYPE_F32) {
+            x[0] = pair(__uint_as_float(raw.x), __uint_as_float(raw.y));
+            x[1] = pair(__uint_as_float(raw.z), __uint_as_float(raw.w));
+        } else {
+            const unsigned w[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
-            for (int k = 0; k < VEC / 4; ++k) widen4<DT>(&raw, k, x + 4 * k);
+            for (int i = 0; i < 4; ++i) {
+                if (DT == FLEXIQ_DTYPE_F16) {
+                    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
+                    x[i] = pair(f.x, f.y);
+                } else {   // bf16: the 16 bits are the top half of an fp32
+                    x[i] = pair(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+                }
+            }
         }
     }
 };
@@ -123,211 +131,275 @@ __device__ __forceinline__ unsigned pack_bf16(float a, float b)
     return *reinterpret_cast<const unsigned *>(&h);
 }
 
-// What a thread keeps of its channels: y = (x - mean) scale + beta.  (x scale + b with the mean in b would round b, by up to 2^-24 |mean| scale: a constant
-// image came out 4e-5 off its beta.)  MANY: the channels belong to several groups, with a mean each.
-template <int VEC, bool MANY> struct Affine {
-    float minus[MANY ? VEC : 1], scale[VEC], beta[VEC];
-    int ent;                  // the slab's entry of their chunk
-    // of channels c .. and their groups' (mean, 1 / deviation)
-    __device__ __forceinline__ void set(const NormArgs &n, int c, const float2 *stat)
-    {
-        if constexpr (VEC == 1) {
-            scale[0] = n.gamma ? n.gamma[c] : 1.f;
-            beta[0] = n.beta ? n.beta[c] : 0.f;
-        } else {
-#pragma unroll
-            for (int i = 0; i < VEC / 4; ++i) {
-                const float4 g = n.gamma ? reinterpret_cast<const float4 *>(n.gamma + c)[i] : make_float4(1.f, 1.f, 1.f, 1.f);
-                const float4 h = n.beta ? reinterpret_cast<const float4 *>(n.beta + c)[i] : make_float4(0.f, 0.f, 0.f, 0.f);
-                scale[4 * i] = g.x; scale[4 * i + 1] = g.y; scale[4 * i + 2] = g.z; scale[4 * i + 3] = g.w;
-                beta[4 * i] = h.x; beta[4 * i + 1] = h.y; beta[4 * i + 2] = h.z; beta[4 * i + 3] = h.w;
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) scale[i] = __fmul_rn(scale[i], stat[MANY ? i : 0].y);
-#pragma unroll
-        for (int i = 0; i < (MANY ? VEC : 1); ++i) minus[i] = -stat[i].x;
-        ent = n.out.y_dtype == FLEXIQ_DTYPE_I8 ? n.out.ent[c >> 4] : 0;
-    }
-};
-// VEC values at channel c of a row, normalised and activated, to where they go
-template <int VEC, bool MANY> __device__ __forceinline__ void finish_values(const NormArgs &n, size_t row, int c, const float *x, const Affine<VEC, MANY> &f)
+// gamma and beta of VEC channels from c on
+template <int VEC> __device__ __forceinline__ void load_affine(const NormArgs &n, int c, pair_t *gamma, pair_t *beta)
 {
-    const NormOut &o = n.out;
-    const int ent = f.ent;
-    float y[VEC];
     if constexpr (VEC == 1) {
-        y[0] = activate_one(n.act, __fmaf_rn(__fadd_rn(x[0], f.minus[0]), f.scale[0], f.beta[0]));
-        const size_t i = row * n.C + c;
-        if (o.y_dtype == FLEXIQ_DTYPE_F32) static_cast<float *>(o.Y)[i] = y[0];
-        else if (o.y_dtype == FLEXIQ_DTYPE_F16) static_cast<__half *>(o.Y)[i] = __float2half_rn(y[0]);
-        else if (o.y_dtype == FLEXIQ_DTYPE_BF16) static_cast<__nv_bfloat16 *>(o.Y)[i] = __float2bfloat16_rn(y[0]);
-        else {
-            unsigned w;
-            quantize_values<1>(o, ent, y, &w);
-            static_cast<int8_t *>(o.Y)[row * n.C + (ent & 0xffffff) * 16 + (c & 15)] = (int8_t)w;
-        }
+        gamma[0] = pair(n.gamma ? n.gamma[c] : 1.f, 1.f);
+        beta[0] = pair(n.beta ? n.beta[c] : 0.f, 0.f);
     } else {
-        pair_t t[VEC / 2];
 #pragma unroll
-        for (int i = 0; i < VEC / 2; ++i)
-            t[i] = fma2(add2(pair(x[2 * i], x[2 * i + 1]), pair(f.minus[MANY ? 2 * i : 0], f.minus[MANY ? 2 * i + 1 : 0])),
-                        pair(f.scale[2 * i], f.scale[2 * i + 1]), pair(f.beta[2 * i], f.beta[2 * i + 1]));
-        activate_n<VEC / 2>(n.act, t);
-#pragma unroll
-        for (int i = 0; i < VEC / 2; ++i) unpair(t[i], &y[2 * i], &y[2 * i + 1]);
-        if (o.y_dtype == FLEXIQ_DTYPE_F32) {
-            float4 *to = reinterpret_cast<float4 *>(static_cast<float *>(o.Y) + row * n.C + c);
-#pragma unroll
-            for (int i = 0; i < VEC / 4; ++i) to[i] = make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
-        } else if (o.y_dtype != FLEXIQ_DTYPE_I8) {
-            unsigned w[VEC / 2];
-            if (o.y_dtype == FLEXIQ_DTYPE_F16) {
-#pragma unroll
-                for (int i = 0; i < VEC / 2; ++i) w[i] = pack_f16(y[2 * i], y[2 * i + 1]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < VEC / 2; ++i) w[i] = pack_bf16(y[2 * i], y[2 * i + 1]);
-            }
-            void *to = static_cast<char *>(o.Y) + (row * n.C + c) * 2;
-            if constexpr (VEC == 8) *static_cast<uint4 *>(to) = make_uint4(w[0], w[1], w[2], w[3]);
-            else *static_cast<uint2 *>(to) = make_uint2(w[0], w[1]);
-        } else {
-            unsigned w[VEC / 4];
-            quantize_values<VEC>(o, ent, y, w);
-            void *to = static_cast<char *>(o.Y) + row * n.C + (ent & 0xffffff) * 16 + (c & 15);
-            if constexpr (VEC == 8) *static_cast<uint2 *>(to) = make_uint2(w[0], w[1]);
-            else *static_cast<unsigned *>(to) = w[0];
+        for (int i = 0; i < VEC / 4; ++i) {
+            const float4 g = n.gamma ? reinterpret_cast<const float4 *>(n.gamma + c)[i] : make_float4(1.f, 1.f, 1.f, 1.f);
+            const float4 h = n.beta ? reinterpret_cast<const float4 *>(n.beta + c)[i] : make_float4(0.f, 0.f, 0.f, 0.f);
+            gamma[2 * i] = pair(g.x, g.y); gamma[2 * i + 1] = pair(g.z, g.w);
+            beta[2 * i] = pair(h.x, h.y); beta[2 * i + 1] = pair(h.z, h.w);
         }
     }
 }
+// What a thread keeps of its channels: y = (x - mean) scale + beta.  (x scale + b with the mean in b would round b, by up to 2^-24 |mean| scale: a constant
+// image came out 4e-5 off its beta.)  MANY: the channels belong to several groups, with a mean each.
+template <int VEC, bool MANY> struct Affine {
+    static constexpr int kPairs = VEC == 1 ? 1 : VEC / 2;
+    pair_t minus[MANY ? kPairs : 1], scale[kPairs], beta[kPairs];
+    // of channels c .. and their groups' (mean, 1 / deviation)
+    __device__ __forceinline__ void set(const NormArgs &n, int c, const float2 *stat)
+    {
+        load_affine<VEC>(n, c, scale, beta);
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) scale[i] = mul2(scale[i], pair(stat[MANY ? 2 * i : 0].y, stat[MANY ? 2 * i + 1 : 0].y));
+#pragma unroll
+        for (int i = 0; i < (MANY ? kPairs : 1); ++i) minus[i] = pair(-stat[MANY ? 2 * i : 0].x, -stat[MANY ? 2 * i + 1 : 0].x);
+    }
+};
+__device__ __forceinline__ int out_bytes(const NormOut &o) { return o.y_dtype == FLEXIQ_DTYPE_F32 ? 4 : o.y_dtype == FLEXIQ_DTYPE_I8 ? 1 : 2; }
+// Where channel c of a row lies in the output, against where it would in the original order
+__device__ __forceinline__ int slab_shift(const NormOut &o, int c, int *ent)
+{
+    if (o.y_dtype != FLEXIQ_DTYPE_I8) return 0;
+    *ent = o.ent[c >> 4];
+    return (*ent & 0xffffff) * 16 + (c & 15) - c;
+}
+// N pieces of normalised values, activated, to at(j) where live(j); ent(j): the slab's entry of their chunk.  One branch for all of them on the
+// activation, and on the output's type.
+template <int VEC, int N, class Live, class At, class Ent>
+__device__ __forceinline__ void store_pieces(const NormArgs &n, pair_t (*t)[VEC == 1 ? 1 : VEC / 2], Live live, At at, Ent ent)
+{
+    const NormOut &o = n.out;
+    constexpr int kPairs = VEC == 1 ? 1 : VEC / 2;
+    activate_n<N * kPairs>(n.act, &t[0][0]);
+    auto each = [&](auto store) {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (live(j)) {
+                float y[2 * kPairs];
+#pragma unroll
+                for (int k = 0; k < kPairs; ++k) unpair(t[j][k], &y[2 * k], &y[2 * k + 1]);
+                store(j, static_cast<char *>(at(j)), y);
+            }
+    };
+    if (o.y_dtype == FLEXIQ_DTYPE_F32)
+        each([](int, char *to, const float *y) {
+            if constexpr (VEC == 1) *reinterpret_cast<float *>(to) = y[0];
+            else {
+#pragma unroll
+                for (int k = 0; k < VEC / 4; ++k) reinterpret_cast<float4 *>(to)[k] = make_float4(y[4 * k], y[4 * k + 1], y[4 * k + 2], y[4 * k + 3]);
+            }
+        });
+    else if (o.y_dtype == FLEXIQ_DTYPE_F16)
+        each([](int, char *to, const float *y) {
+            if constexpr (VEC == 1) *reinterpret_cast<__half *>(to) = __float2half_rn(y[0]);
+            else if constexpr (VEC == 4) *reinterpret_cast<uint2 *>(to) = make_uint2(pack_f16(y[0], y[1]), pack_f16(y[2], y[3]));
+            else *reinterpret_cast<uint4 *>(to) = make_uint4(pack_f16(y[0], y[1]), pack_f16(y[2], y[3]), pack_f16(y[4], y[5]), pack_f16(y[6], y[7]));
+        });
+    else if (o.y_dtype == FLEXIQ_DTYPE_BF16)
+        each([](int, char *to, const float *y) {
+            if constexpr (VEC == 1) *reinterpret_cast<__nv_bfloat16 *>(to) = __float2bfloat16_rn(y[0]);
+            else if constexpr (VEC == 4) *reinterpret_cast<uint2 *>(to) = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
+            else *reinterpret_cast<uint4 *>(to) = make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
+        });
+    else
+        each([&](int j, char *to, const float *y) {
+            unsigned w[(VEC + 3) / 4];
+            quantize_values<VEC>(o, ent(j), y, w);
+            if constexpr (VEC == 1) *to = (char)w[0];
+            else if constexpr (VEC == 4) *reinterpret_cast<unsigned *>(to) = w[0];
+            else *reinterpret_cast<uint2 *>(to) = make_uint2(w[0], w[1]);
+        });
+}
+template <int VEC, bool MANY> __device__ __forceinline__ void normalise(pair_t *x, const Affine<VEC, MANY> &f)
+{
+#pragma unroll
+    for (int i = 0; i < Affine<VEC, MANY>::kPairs; ++i) x[i] = fma2(add2(x[i], f.minus[MANY ? i : 0]), f.scale[i], f.beta[i]);
+}
+
 __device__ __forceinline__ float warp_sum(float v)
 {
 #pragma unroll
     for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
     return v;
 }
-__device__ __forceinline__ float deviation_inverse(float M2, float n, float eps) { return __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(__fdiv_rn(M2, n), eps))); }
-
-// Mean and M2 of one run of values: tile by tile, joined as above
-struct Moments {
-    float n, mean, M2;
-    __device__ __forceinline__ void join(float nb, float mb, float Mb)
-    {
-        const float all = n + nb, d = mb - mean, share = n > 0.f ? __fdiv_rn(nb, all) : 1.f;
-        mean = __fmaf_rn(d, share, mean);
-        M2 = __fadd_rn(M2, __fmaf_rn(__fmul_rn(d, d), __fmul_rn(n, share), Mb));
-        n = all;
-    }
-};
-
-// Sums and then squared deviations of the values of NV pieces, `valid` bit by bit; MANY: each channel of the piece apart.  Returns the pieces counted.
-template <int DT, int VEC, int NV, bool MANY>
-__device__ __forceinline__ int piece_moments(const Piece<DT, VEC> *v, unsigned valid, float *mean, float *M2)
+// over `width` lanes (a power of two) side by side
+__device__ __forceinline__ float part_sum(float v, int width)
 {
-    constexpr int S = MANY ? VEC : 1;
-    const int cnt = __popc(valid);
-    float s[S] = {};
+    for (int d = width >> 1; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    return v;
+}
+__device__ __forceinline__ float both(pair_t p)
+{
+    float a, b;
+    unpair(p, &a, &b);
+    return a + b;
+}
+template <int N> __device__ __forceinline__ float fold(const pair_t *p)
+{
+    float s = both(p[0]);
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
-        if (valid >> j & 1) {
-            float x[VEC];
-            v[j].widen(x);
-            if (MANY) {
+    for (int i = 1; i < N; ++i) s += both(p[i]);
+    return s;
+}
+// (two units in the last place at most)
+__device__ __forceinline__ float deviation_inverse(float M2, float n, float eps) { return rsqrtf(__fadd_rn(__fdividef(M2, n), eps)); }
+
+__device__ __forceinline__ int quotient(int n, unsigned inverse) { return inverse ? (int)__umulhi((unsigned)n, inverse) : n; }   // (0 stands for 2^32: by one)
+
+struct Moments { float n, mean, M2; };
+// s / n, one rounding off at most and exact where it can be (the mean of equal values is that value): a product corrected by its remainder
+__device__ __forceinline__ pair_t divide(pair_t s, pair_t minus_n, pair_t inverse)
+{
+    const pair_t m = mul2(s, inverse);
+    return fma2(fma2(m, minus_n, s), inverse, m);
+}
+__device__ __forceinline__ float divide(float s, float n, float inverse)
+{
+    const float m = __fmul_rn(s, inverse);
+    return __fmaf_rn(__fmaf_rn(-m, n, s), inverse, m);
+}
+// Sums of pairs per channel -> means, of each channel (MANY) or of all
+template <int VEC, bool MANY> __device__ __forceinline__ void means_of(const pair_t *s, int pieces, float *mean)
+{
+    const float n = (float)(pieces ? pieces * (MANY ? 1 : VEC) : 1), inverse = __frcp_rn(n);
+    constexpr int kPairs = VEC == 1 ? 1 : VEC / 2;
+    if (MANY) {
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) s[i % S] += x[i];
-            } else {
+        for (int i = 0; i < kPairs; ++i) unpair(divide(s[i], pair(-n, -n), pair(inverse, inverse)), &mean[(2 * i) % VEC], &mean[(2 * i + 1) % VEC]);
+    } else {
+        mean[0] = divide(fold<kPairs>(s), n, inverse);
+    }
+}
+template <int VEC, bool MANY> __device__ __forceinline__ void minus_means(const float *mean, pair_t *m)
+{
 #pragma unroll
-                for (int w = VEC / 2; w; w >>= 1)
+    for (int i = 0; i < (MANY ? VEC / 2 : 1); ++i) m[i] = pair(-mean[MANY ? 2 * i : 0], VEC == 1 ? 0.f : -mean[MANY ? 2 * i + 1 : 0]);
+}
+template <int VEC, bool MANY> __device__ __forceinline__ void squares_of(const pair_t *q, float *M2)
+{
+    constexpr int kPairs = VEC == 1 ? 1 : VEC / 2;
+    if (MANY) {
 #pragma unroll
-                    for (int i = 0; i < w; ++i) x[i] += x[i + w];
-                s[0] += x[0];
-            }
-        }
-    const float count = (float)(cnt ? cnt * (MANY ? 1 : VEC) : 1);   // (divided by, not multiplied by an inverse: the mean of equal values is that value)
-#pragma unroll
-    for (int i = 0; i < S; ++i) { mean[i] = __fdiv_rn(s[i], count); M2[i] = 0.f; }
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-        if (valid >> j & 1) {
-            float x[VEC];
-            v[j].widen(x);
-            if (MANY) {
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) { const float d = x[i] - mean[i % S]; M2[i % S] = __fmaf_rn(d, d, M2[i % S]); }
-            } else {
-                float q = 0.f;
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) { const float d = x[i] - mean[0]; q = __fmaf_rn(d, d, q); }
-                M2[0] += q;
-            }
-        }
-    return cnt;
+        for (int i = 0; i < kPairs; ++i) unpair(q[i], &M2[(2 * i) % VEC], &M2[(2 * i + 1) % VEC]);
+    } else {
+        M2[0] = fold<kPairs>(q);
+    }
 }
 
-// What the threads of a block found -> their groups' moments in gstat[0 .. gpb): a warp per group over the entries of its threads (its channels').
+__device__ unsigned int g_norm_status = 0;
+
+// What the threads of a block found -> their groups' moments in gstat[0 .. gpb): some lanes per group over its threads' entries.  MANY: a thread has `sub`
+// entries, one for each group its piece holds where those are whole, else one for each channel.
 template <int VEC, bool MANY>
-__device__ __forceinline__ void block_moments(const NormArgs &a, float *red_mean, float *red_M2, const float *red_n, Moments *gstat)
+__device__ __forceinline__ void block_moments(const NormArgs &a, const float *red_mean, const float *red_M2, const float *red_n, Moments *gstat, int sub_entries)
 {
-    constexpr int S = MANY ? VEC : 1;
     __syncthreads();
-    const int warps = blockDim.x >> 5, lane = threadIdx.x & 31;
-    const int pitch = a.cpt > 1 ? (int)blockDim.x : a.nch * S, each = a.cpt > 1 ? (int)blockDim.x : (MANY ? a.cpg : a.cpg / VEC);   // entries of a position, and of a group among them
-    for (int g = threadIdx.x >> 5; g < a.gpb; g += warps) {
-        const int total = a.lanes * each, first = g * each;
-        const float ref = red_mean[first];
-        float n = 0.f, d = 0.f;
-        for (int i = lane; i < total; i += 32) {
-            const int row = i / each, e = row * pitch + first + (i - row * each);
-            const float w = red_n[MANY ? e / S : e];
+    const int warps = blockDim.x >> 5;
+    int width = 32;                                   // lanes per group: fewer where there are more groups than warps
+    while (width > 4 && warps * (32 / width) < a.gpb) width >>= 1;
+    const int sub = threadIdx.x & (width - 1), step = blockDim.x >> (31 - __clz(width)), sub_log = 31 - __clz(sub_entries);
+    // entries of a position, and of a group among them
+    const int pitch = a.cpt > 1 ? (int)blockDim.x : a.nch * sub_entries, each = a.cpt > 1 ? (int)blockDim.x : MANY ? (sub_entries < VEC ? 1 : a.cpg) : a.cpg / VEC;
+    const int jump = quotient(width, a.by_each), rest = width - jump * each, row0 = quotient(sub, a.by_each), in0 = sub - row0 * each;
+    for (int g0 = 0; g0 < a.gpb; g0 += step) {        // (all lanes stay: the sums need them)
+        const int g = g0 + (int)(threadIdx.x >> (31 - __clz(width)));
+        const int rows = g < a.gpb ? a.lanes : 0, first = g < a.gpb ? g * each : 0;
+        auto over = [&](auto take) {
+            for (int row = row0, in = in0; row < rows;) {
+                const int e = row * pitch + first + in;
+                take(MANY ? red_n[e >> sub_log] : red_n[e], e);
+                row += jump;
+                in += rest;
+                if (in >= each) { in -= each; ++row; }
+            }
+        };
+        float n = 0.f, d = 0.f, M2 = 0.f, c = 0.f;
+        over([&](float w, int e) {
             n += w;
-            d = __fmaf_rn(w, red_mean[e] - ref, d);
-        }
-        n = warp_sum(n);
-        d = warp_sum(d);
-        const float mean = n > 0.f ? ref + __fdiv_rn(d, n) : 0.f;
-        float M2 = 0.f;
-        for (int i = lane; i < total; i += 32) {
-            const int row = i / each, e = row * pitch + first + (i - row * each);
-            const float w = red_n[MANY ? e / S : e], q = red_mean[e] - mean;
-            if (w > 0.f) M2 += __fmaf_rn(w * q, q, red_M2[e]);
-        }
-        M2 = warp_sum(M2);
-        if (lane == 0) gstat[g] = Moments{n, mean, M2};
+            d = __fmaf_rn(w, red_mean[e], d);
+        });
+        n = part_sum(n, width);
+        d = part_sum(d, width);
+        const float mean = n > 0.f ? __fdiv_rn(d, n) : 0.f;
+        over([&](float w, int e) {
+            const float q = red_mean[e] - mean, wq = w * q;
+            c += wq;
+            M2 += __fmaf_rn(wq, q, red_M2[e]);             // (a thread without values: all zero)
+        });
+        M2 = part_sum(M2, width);
+        c = part_sum(c, width);
+        if (sub == 0 && g < a.gpb) gstat[g] = Moments{n, n > 0.f ? mean + __fdividef(c, n) : 0.f, M2};
     }
     __syncthreads();
 }
+// A thread's moments to its entries (the array's size: kNormThreads * VEC for MANY).  Returns the entries of a thread.
+template <int VEC, bool MANY>
+__device__ __forceinline__ int put_moments(const NormArgs &a, const float *mean, const float *M2, float pieces, float *red_mean, float *red_M2, float *red_n)
+{
+    const int t = threadIdx.x;
+    if (!MANY) {
+        red_mean[t] = mean[0];
+        red_M2[t] = M2[0];
+        red_n[t] = pieces * VEC;
+        return 1;
+    }
+    if (VEC % a.cpg == 0) {                            // whole groups of 1, 2 (or 4) channels: joined here
+        auto whole = [&](auto cpg) {
+            constexpr int W = decltype(cpg)::value;
+#pragma unroll
+            for (int g = 0; g < VEC / W; ++g) {
+                float d = 0.f, M = 0.f;
+#pragma unroll
+                for (int i = 1; i < W; ++i) d += mean[g * W + i] - mean[g * W];
+                const float centre = __fmaf_rn(d, 1.0f / W, mean[g * W]);
+#pragma unroll
+                for (int i = 0; i < W; ++i) { const float o = mean[g * W + i] - centre; M += __fmaf_rn(pieces * o, o, M2[g * W + i]); }
+                red_mean[t * (VEC / W) + g] = centre;
+                red_M2[t * (VEC / W) + g] = pieces > 0.f ? M : 0.f;
+            }
+            red_n[t] = pieces * W;
+            return VEC / W;
+        };
+        if (a.cpg == 2) return whole(std::integral_constant<int, 2>{});
+        if (VEC == 8 && a.cpg == 4) return whole(std::integral_constant<int, VEC == 8 ? 4 : 2>{});
+    }
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) { red_mean[t * VEC + i] = mean[i]; red_M2[t * VEC + i] = M2[i]; }
+    red_n[t] = pieces;
+    return VEC;
+}
 
-// Which pieces a thread has: piece j of its positions
-struct Pieces {
-    int col, pl;        // its column and position side by side; cpt > 1: its first column, position 0
+// A thread's pieces: its column and its position among those side by side; cpt > 1: its first column, at every position
+struct Place {
+    int col, pl, cols;        // cols: columns of a position that are its own (cpt > 1)
     bool live;
-    __device__ __forceinline__ Pieces(const NormArgs &a)
+    __device__ __forceinline__ Place(const NormArgs &a)
     {
         const int t = threadIdx.x;
-        if (a.cpt > 1) { pl = 0; col = t; live = true; }
-        else { pl = t / a.nch; col = t - pl * a.nch; live = pl < a.lanes; }
+        if (a.cpt > 1) { pl = 0; col = t; cols = (a.nch - t + (int)blockDim.x - 1) / (int)blockDim.x; live = t < a.nch; }
+        else { pl = quotient(t, a.by_nch); col = t - pl * a.nch; cols = 1; live = pl < a.lanes; }
     }
-    // (position, column) of the thread's piece j, walked in order
-    struct Walk {
-        int p, c, k;
-    };
-    __device__ __forceinline__ Walk begin() const { return Walk{pl, col, 0}; }
-    __device__ __forceinline__ void next(const NormArgs &a, Walk &w) const
+    // its pieces among `positions` (fewer than 2^16: by a multiplication)
+    __device__ __forceinline__ int count(const NormArgs &a, int positions) const
     {
-        if (a.cpt > 1) {
-            w.c += blockDim.x;
-            if (++w.k == a.cpt) { w.k = 0; w.c = col; ++w.p; }
-        } else {
-            w.p += a.lanes;
-        }
+        if (!live || positions <= pl) return 0;
+        if (a.cpt > 1) return positions * cols;
+        const int n = positions - pl + a.lanes - 1;
+        return n < 65536 ? quotient(n, a.by_lanes) : n / a.lanes;
     }
 };
 
 // (mean, 1 / deviation) of the channels of column `col` (MANY: of each)
 template <int VEC, bool MANY> __device__ __forceinline__ void column_stats(const NormArgs &a, int col, const float2 *fin, float2 *stat)
 {
-    int g = col * VEC / a.cpg, left = a.cpg - (col * VEC - g * a.cpg);
+    int g = quotient(col * VEC, a.by_cpg), left = a.cpg - (col * VEC - g * a.cpg);
     stat[0] = fin[g];
 #pragma unroll
     for (int i = 1; i < (MANY ? VEC : 1); ++i) {
@@ -336,341 +408,606 @@ template <int VEC, bool MANY> __device__ __forceinline__ void column_stats(const
     }
 }
 
-// "held": block rank `blockIdx.x % cluster` of an image's channel block
-template <int DT, int VEC, int NV, bool MANY>
-__global__ void __launch_bounds__(kNormThreads, NV <= 4 ? 4 : 2) group_norm_held_kernel(const NormArgs a)
+// A thread's pieces through shared memory, NV at a time and DEPTH - 1 batches ahead: its own slots, [batch][piece][thread], so it waits for no one else.
+template <int DT, int VEC, int NV, int DEPTH> struct PieceRing {
+    typedef Piece<DT, VEC> P;
+    typename P::Raw *hold;
+    const char *from;
+    size_t apart;             // bytes from one piece to the next
+    int left;                 // pieces not asked for yet
+    int slot;                 // (the first piece's place)
+    static constexpr int T = kNormThreads, kBatch = NV * T;
+    __device__ __forceinline__ PieceRing(void *smem, const char *from_, size_t apart_, int cnt_)
+        : hold(static_cast<typename P::Raw *>(smem) + threadIdx.x), from(from_), apart(apart_), left(cnt_), slot(0)
+    {
+        for (int k = 0; k < DEPTH - 1; ++k) ask(k * kBatch);
+    }
+    __device__ __forceinline__ void one(int at)
+    {
+        if constexpr (VEC == 1) {
+            P v;
+            v.load(from);
+            hold[at] = v.raw;
+        } else {
+            ptx::cp_async_16(ptx::smem_u32(&hold[at]), from);
+        }
+        from += apart;
+    }
+    __device__ __forceinline__ void ask(int to)           // (an empty batch of copies where there is nothing left)
+    {
+        if (left >= NV) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j) one(to + j * T);
+            left -= NV;
+        } else {
+            for (int at = to; left > 0; --left, at += T) one(at);
+        }
+        ptx::cp_async_commit();
+    }
+    // the next batch is here; the one DEPTH - 1 behind it is asked for (into the slots read last)
+    __device__ __forceinline__ void turn()
+    {
+        ask(slot == 0 ? (DEPTH - 1) * kBatch : slot - kBatch);
+        ptx::cp_async_wait_but<DEPTH - 1>();
+    }
+    __device__ __forceinline__ P piece(int j) const
+    {
+        P v;
+        v.raw = hold[slot + j * T];
+        return v;
+    }
+    __device__ __forceinline__ void done()
+    {
+        slot = slot == (DEPTH - 1) * kBatch ? 0 : slot + kBatch;
+    }
+};
+
+// "held": block rank `blockIdx.x % cluster` of an image's channel block.  A thread's pieces lie in shared memory, [piece][thread]: in registers
+// the loops over them had to be unrolled, and fetching some thousands of instructions once each cost more than the memory.
+template <int DT, int VEC, bool MANY, int T>
+__global__ void __launch_bounds__(T, 1024 / T) group_norm_held_kernel(const NormArgs a)
 {
-    constexpr int S = MANY ? VEC : 1;
-    __shared__ float red_mean[kNormThreads * S], red_M2[kNormThreads * S], red_n[kNormThreads];
+    constexpr int S = MANY ? VEC : 1, kPairs = VEC == 1 ? 1 : VEC / 2, kNext = T * (VEC == 1 ? 4 : 16);
+    typedef Piece<DT, VEC> P;
+    extern __shared__ __align__(16) uint8_t hold_bytes[];
+    __shared__ float red_mean[T * S], red_M2[T * S], red_n[T];
     __shared__ Moments gstat[kMaxGroups];
-    __shared__ float2 fin[kMaxGroups];
-    const int blocks = a.groups / a.gpb;                       // channel blocks
-    const unsigned unit = blockIdx.x / (unsigned)a.cluster;
-    const int rank = (int)(blockIdx.x - unit * (unsigned)a.cluster);
-    const long long img = unit / (unsigned)blocks;
-    const int c0 = (int)(unit - (unsigned)img * (unsigned)blocks) * a.gpb * a.cpg;
+    __shared__ float2 fin[kMaxGroups], inbox[kNormCluster][kMaxGroups];
+    __shared__ uint64_t arrived;
+    // The blocks of a cluster write their groups' moments into one another's shared memory.  First each has to know that the others have begun
+    // and their barriers stand: that is waited for below, while the data comes.  (Reading them from the others between two barriers
+    // of the cluster was FIGURES slower.)
+    if (a.cluster_log) {
+        if (threadIdx.x == 0) {
+            ptx::mbar_init(&arrived, 1);
+            ptx::fence_mbar_init();
+            ptx::mbar_expect_tx(&arrived, (unsigned)(a.gpb << a.cluster_log) * 8u);
+        }
+        __syncthreads();
+        ptx::cluster_arrive();
+    }
+    // block (image and rank in the cluster, channel block)
+    const int rank = (int)(blockIdx.x & ((1u << a.cluster_log) - 1u));
+    const long long img = blockIdx.x >> a.cluster_log;
+    const int c0 = (int)blockIdx.y * a.gpb * a.cpg;
     const long long p0 = rank * a.span, left = a.P - p0;
     const int mine = (int)(left < 0 ? 0 : left < a.span ? left : a.span);
-    const size_t row0 = (size_t)img * a.P + p0;
-    const Pieces who(a);
+    const Place who(a);
+    const int cnt = who.count(a, mine);
+    // element of piece j: one position after another (cpt > 1: its columns of a position first)
+    const size_t e0 = ((size_t)img * a.P + p0 + who.pl) * a.C + c0 + (size_t)who.col * VEC;
+    const size_t step = (size_t)a.lanes * a.C;
+    const bool wide = a.cpt > 1;
+    auto element = [&](int j) { return e0 + (size_t)(j / who.cols) * a.C + (size_t)(j % who.cols) * T * VEC; };   // (wide)
+    uint8_t *const hold = hold_bytes + threadIdx.x * (VEC == 1 ? 4 : 16);
     ptx::pdl_wait();
-    Piece<DT, VEC> v[NV];
-    unsigned valid = 0;
     {
-        Pieces::Walk w = who.begin();
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            if (who.live && w.p < mine && w.c < a.nch) {
-                v[j].load(a.X, (row0 + w.p) * a.C + c0 + w.c * VEC);
-                valid |= 1u << j;
+        const char *from = static_cast<const char *>(a.X) + e0 * P::kBytes;
+        const size_t next = step * P::kBytes;
+        uint8_t *to = hold;
+#pragma unroll 4
+        for (int j = 0; j < cnt; ++j) {
+            if (wide) from = static_cast<const char *>(a.X) + element(j) * P::kBytes;
+            if constexpr (VEC == 1) {
+                P v;
+                v.load(from);
+                *reinterpret_cast<float *>(to) = v.raw;
+            } else {
+                ptx::cp_async_16(ptx::smem_u32(to), from);
             }
-            who.next(a, w);
+            from += next;
+            to += kNext;
         }
+        ptx::cp_async_wait();                                  // (each thread reads what it asked for itself)
     }
+    auto piece = [&](const uint8_t *at, pair_t *x) {
+        P v;
+        v.raw = *reinterpret_cast<const typename P::Raw *>(at);
+        v.widen(x);
+    };
     float mean[S], M2[S];
-    const int cnt = piece_moments<DT, VEC, NV, MANY>(v, valid, mean, M2);
+    {
+        pair_t s[kPairs] = {}, m[MANY ? kPairs : 1];
+        const uint8_t *at = hold;
+#pragma unroll 4
+        for (int j = 0; j < cnt; ++j, at += kNext) {
+            pair_t x[kPairs];
+            piece(at, x);
 #pragma unroll
-    for (int i = 0; i < S; ++i) { red_mean[threadIdx.x * S + i] = mean[i]; red_M2[threadIdx.x * S + i] = M2[i]; }
-    red_n[threadIdx.x] = (float)(cnt * (MANY ? 1 : VEC));
-    block_moments<VEC, MANY>(a, red_mean, red_M2, red_n, gstat);
-    if (a.cluster > 1) {
-        ptx::cluster_sync_all();
-        for (int g = threadIdx.x; g < a.gpb; g += blockDim.x) {
-            float n[kNormCluster], m[kNormCluster], q[kNormCluster];
+            for (int i = 0; i < kPairs; ++i) s[i] = add2(s[i], x[i]);
+        }
+        means_of<VEC, MANY>(s, cnt, mean);
+        minus_means<VEC, MANY>(mean, m);
+        pair_t q[kPairs] = {};
+        at = hold;
+#pragma unroll 4
+        for (int j = 0; j < cnt; ++j, at += kNext) {
+            pair_t x[kPairs];
+            piece(at, x);
 #pragma unroll
-            for (int r = 0; r < kNormCluster; ++r) {
-                n[r] = m[r] = q[r] = 0.f;
-                if (r < a.cluster) {
-                    const uint32_t at = ptx::mapa(ptx::smem_u32(&gstat[g]), (uint32_t)r);
-                    n[r] = __uint_as_float(ptx::ld_shared_cluster(at));
-                    m[r] = __uint_as_float(ptx::ld_shared_cluster(at + 4));
-                    q[r] = __uint_as_float(ptx::ld_shared_cluster(at + 8));
-                }
-            }
-            float all = 0.f, d = 0.f, M = 0.f;
-#pragma unroll
-            for (int r = 0; r < kNormCluster; ++r) { all += n[r]; d = __fmaf_rn(n[r], m[r] - m[0], d); }
-            const float centre = m[0] + __fdiv_rn(d, all);
-#pragma unroll
-            for (int r = 0; r < kNormCluster; ++r) { const float o = m[r] - centre; if (n[r] > 0.f) M += __fmaf_rn(n[r] * o, o, q[r]); }
-            fin[g] = make_float2(centre, deviation_inverse(M, all, a.eps));
+            for (int i = 0; i < kPairs; ++i) { x[i] = add2(x[i], m[MANY ? i : 0]); q[i] = fma2(x[i], x[i], q[i]); }
+        }
+        squares_of<VEC, MANY>(q, M2);
+    }
+    block_moments<VEC, MANY>(a, red_mean, red_M2, red_n, gstat, put_moments<VEC, MANY>(a, mean, M2, (float)cnt, red_mean, red_M2, red_n));
+    if (a.cluster_log) {
+        // a thread per group and block of the cluster, those of a group side by side
+        const int k = 1 << a.cluster_log, per = T >> a.cluster_log, r = threadIdx.x & (k - 1);
+        ptx::cluster_wait();
+        const uint32_t bar = ptx::mapa(ptx::smem_u32(&arrived), (uint32_t)r);
+        for (int g = (int)(threadIdx.x >> a.cluster_log); g < a.gpb; g += per)
+            ptx::st_async_64(ptx::mapa(ptx::smem_u32(&inbox[rank][g]), (uint32_t)r), gstat[g].mean, gstat[g].M2, bar);
+        bool here = ptx::mbar_try_wait(&arrived, 0);
+        for (uint32_t i = 0; i < (1u << 21) && !here; ++i) here = ptx::mbar_try_wait_hint_s(ptx::smem_u32(&arrived), 0, 1000u);   // (parked for a microsecond at most)
+        if (!here) atomicMax(&g_norm_status, 0x401u);
+        const long long other = a.P - r * a.span;              // positions of block r
+        const float n = (float)((other < 0 ? 0 : other < a.span ? (int)other : (int)a.span) * a.cpg), all = (float)(a.P * a.cpg);
+        for (int g0 = 0; g0 < a.gpb; g0 += per) {              // (all lanes stay: the sums need them)
+            const int g = g0 + (int)(threadIdx.x >> a.cluster_log);
+            const float2 s = inbox[r][g < a.gpb ? g : 0];
+            const float centre = __fdiv_rn(part_sum(__fmul_rn(n, s.x), k), all), o = s.x - centre, no = n * o;
+            const float M = part_sum(__fmaf_rn(no, o, s.y), k), c = part_sum(no, k);
+            if (r == 0 && g < a.gpb) fin[g] = make_float2(centre + __fdividef(c, all), deviation_inverse(M, all, a.eps));
         }
     } else {
-        for (int g = threadIdx.x; g < a.gpb; g += blockDim.x) fin[g] = make_float2(gstat[g].mean, deviation_inverse(gstat[g].M2, gstat[g].n, a.eps));
+        for (int g = threadIdx.x; g < a.gpb; g += T) fin[g] = make_float2(gstat[g].mean, deviation_inverse(gstat[g].M2, gstat[g].n, a.eps));
     }
     ptx::pdl_launch_dependents();
     __syncthreads();
-    if (a.cluster > 1) ptx::cluster_arrive();                  // this block has read what it needs of the others
-    if (valid) {
-        float2 stat[MANY ? VEC : 1];
+    if (cnt) {
+        float2 stat[S];
         Affine<VEC, MANY> f;
-        Pieces::Walk w = who.begin();
-        auto column = [&]() {
-            column_stats<VEC, MANY>(a, a.cpt > 1 ? 0 : w.c, fin, stat);   // (cpt > 1: one group)
-            f.set(a, c0 + w.c * VEC, stat);
-        };
-        column();
+        int ent = 0;
+        const int ob = out_bytes(a.out);
+        column_stats<VEC, MANY>(a, wide ? 0 : who.col, fin, stat);   // (wide: one group)
+        const uint8_t *at = hold;
+        if (!wide) {
+            constexpr int NV = 2;
+            const int c = c0 + who.col * VEC;
+            f.set(a, c, stat);
+            char *to = static_cast<char *>(a.out.Y) + (e0 + slab_shift(a.out, c, &ent)) * ob;
+            const size_t far = step * ob;
+            auto batch = [&](auto whole, int n) {              // (what is not there is not stored)
+                pair_t x[NV][kPairs];
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            if (valid >> j & 1) {
-                if (a.cpt > 1 && j) column();
-                float x[VEC];
-                v[j].widen(x);
-                finish_values(a, row0 + w.p, c0 + w.c * VEC, x, f);
+                for (int j = 0; j < NV; ++j)
+                    if (decltype(whole)::value || j < n) piece(at + j * kNext, x[j]);
+                    else {
+#pragma unroll
+                        for (int i = 0; i < kPairs; ++i) x[j][i] = pair(0.f, 0.f);
+                    }
+#pragma unroll
+                for (int j = 0; j < NV; ++j) normalise<VEC, MANY>(x[j], f);
+                store_pieces<VEC, NV>(a, x, [&](int j) { return decltype(whole)::value || j < n; }, [&](int) { char *const here = to; to += far; return here; }, [&](int) { return ent; });
+                at += NV * kNext;
+            };
+            int j = 0;
+#pragma unroll 1
+            for (; j + NV <= cnt; j += NV) batch(std::true_type{}, NV);
+            if (j < cnt) batch(std::false_type{}, cnt - j);
+        } else {
+#pragma unroll 1
+            for (int j = 0; j < cnt; ++j, at += kNext) {
+                const int c = c0 + (who.col + (j % who.cols) * T) * VEC;
+                f.set(a, c, stat);
+                char *to = static_cast<char *>(a.out.Y) + (element(j) + slab_shift(a.out, c, &ent)) * ob;
+                pair_t x[1][kPairs];
+                piece(at, x[0]);
+                normalise<VEC, MANY>(x[0], f);
+                store_pieces<VEC, 1>(a, x, [](int) { return true; }, [&](int) { return to; }, [&](int) { return ent; });
             }
-            who.next(a, w);
         }
     }
-    __syncwarp();
-    if (a.cluster > 1) ptx::cluster_wait();                    // the others have read what they need of this one
 }
 
+constexpr int kStatsPieces = 8, kStatsDepth = 2, kApplyPieces = 4, kApplyDepth = 3;
 // "twice", the first: moments of a piece of an image's channel block
 template <int DT, int VEC, bool MANY>
 __global__ void __launch_bounds__(kNormThreads, 2) group_norm_stats_kernel(const NormArgs a)
 {
-    constexpr int S = MANY ? VEC : 1, NV = 8;
+    constexpr int S = MANY ? VEC : 1, kPairs = VEC == 1 ? 1 : VEC / 2, NV = kStatsPieces;
+    typedef Piece<DT, VEC> P;
+    extern __shared__ __align__(16) uint8_t hold_bytes[];
     __shared__ float red_mean[kNormThreads * S], red_M2[kNormThreads * S], red_n[kNormThreads];
     __shared__ Moments gstat[kMaxGroups];
-    const int blocks = a.groups / a.gpb;
-    const unsigned unit = blockIdx.x / (unsigned)a.cluster;
-    const int piece = (int)(blockIdx.x - unit * (unsigned)a.cluster);
-    const long long img = unit / (unsigned)blocks;
-    const int block = (int)(unit - (unsigned)img * (unsigned)blocks), c0 = block * a.gpb * a.cpg;
-    const long long p0 = piece * a.span, left = a.P - p0, mine = left < 0 ? 0 : left < a.span ? left : a.span;
-    const size_t row0 = (size_t)img * a.P + p0;
-    const Pieces who(a);
+    // block (image and piece, channel block)
+    const long long img = blockIdx.x / (unsigned)a.cluster;
+    const int part = (int)(blockIdx.x - (unsigned)img * (unsigned)a.cluster), block = (int)blockIdx.y, c0 = block * a.gpb * a.cpg;
+    const long long p0 = part * a.span, left = a.P - p0;
+    const int mine = (int)(left < 0 ? 0 : left < a.span ? left : a.span);
+    const Place who(a);
+    const size_t e0 = ((size_t)img * a.P + p0 + who.pl) * a.C + c0 + (size_t)who.col * VEC;
+    const bool wide = a.cpt > 1;
+    const int cnt = who.count(a, mine);
+    const size_t step = (size_t)a.lanes * a.C * P::kBytes;
     ptx::pdl_wait();
-    Moments sum[S];
+    // One pass: sums of x - K and of its square, K the mean of the thread's first pieces (of each channel: MANY).  Their squares' sum is at most
+    // 1 + n / NV^2 times what is left of it when the mean is taken out, however far one of the first values lies, since that one is among them; NV
+    // n pieces are summed apart before they are added to the rest, so no sum has more than some sixty roundings.
+    const char *from = static_cast<const char *>(a.X) + e0 * P::kBytes;
+    pair_t K[MANY ? kPairs : 1], S1[kPairs] = {}, S2[kPairs] = {};
+    float shift[S] = {};
+    bool first = true;
+    int batches = 0;
+    pair_t s[kPairs] = {}, q[kPairs] = {};
+    auto tile = [&](auto piece, int pieces, auto all) {      // `all`: every piece of the tile is there
+        if (first) {
+            pair_t t[kPairs] = {};
 #pragma unroll
-    for (int i = 0; i < S; ++i) sum[i] = Moments{0.f, 0.f, 0.f};
-    const int tile = a.cpt > 1 ? 1 : a.lanes * NV;             // positions a step (cpt > 1: NV of a position's pieces a step)
-    for (long long base = 0; base < mine; base += tile) {
-        for (int k0 = 0; k0 < a.cpt; k0 += NV) {
-            Piece<DT, VEC> v[NV];
-            unsigned valid = 0;
+            for (int j = 0; j < NV; ++j)
+                if (decltype(all)::value || j < pieces) {
+                    pair_t x[kPairs];
+                    piece(j).widen(x);
+#pragma unroll
+                    for (int i = 0; i < kPairs; ++i) t[i] = add2(t[i], x[i]);
+                }
+            means_of<VEC, MANY>(t, pieces, shift);
+            minus_means<VEC, MANY>(shift, K);
+            first = false;
+        }
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            if (decltype(all)::value || j < pieces) {
+                pair_t x[kPairs];
+                piece(j).widen(x);
+#pragma unroll
+                for (int i = 0; i < kPairs; ++i) { x[i] = add2(x[i], K[MANY ? i : 0]); s[i] = add2(s[i], x[i]); q[i] = fma2(x[i], x[i], q[i]); }
+            }
+        if ((++batches & 3) == 0) {
+#pragma unroll
+            for (int i = 0; i < kPairs; ++i) { S1[i] = add2(S1[i], s[i]); S2[i] = add2(S2[i], q[i]); s[i] = q[i] = pair(0.f, 0.f); }
+        }
+    };
+    if (!wide) {
+        PieceRing<DT, VEC, NV, kStatsDepth> ring(hold_bytes, from, step, cnt);
+        auto piece = [&](int j) { return ring.piece(j); };
+        int todo = cnt;
+        for (; todo >= NV; todo -= NV) {
+            ring.turn();
+            tile(piece, NV, std::true_type{});
+            ring.done();
+        }
+        if (todo) {
+            ring.turn();
+            tile(piece, todo, std::false_type{});
+        }
+    } else {
+        for (int j0 = 0; j0 < cnt; j0 += NV) {
+            P v[NV];
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
-                const long long p = base + (a.cpt > 1 ? 0 : who.pl + j * a.lanes);
-                const int c = a.cpt > 1 ? who.col + (k0 + j) * (int)blockDim.x : who.col;
-                if (who.live && p < mine && c < a.nch) {
-                    v[j].load(a.X, (row0 + p) * a.C + c0 + c * VEC);
-                    valid |= 1u << j;
-                }
+                const int p = (j0 + j) / who.cols;
+                if (j0 + j < cnt) v[j].load(from + ((size_t)p * a.C + (size_t)(j0 + j - p * who.cols) * blockDim.x * VEC) * P::kBytes);
             }
-            float mean[S], M2[S];
-            const float n = (float)(piece_moments<DT, VEC, NV, MANY>(v, valid, mean, M2) * (MANY ? 1 : VEC));
-#pragma unroll
-            for (int i = 0; i < S; ++i) sum[i].join(n, mean[i], M2[i]);
+            tile([&](int j) { return v[j]; }, cnt - j0 < NV ? cnt - j0 : NV, std::false_type{});
         }
     }
+    float mean[S], M2[S];
+    {
 #pragma unroll
-    for (int i = 0; i < S; ++i) { red_mean[threadIdx.x * S + i] = sum[i].mean; red_M2[threadIdx.x * S + i] = sum[i].M2; }
-    red_n[threadIdx.x] = sum[0].n;
+        for (int i = 0; i < kPairs; ++i) { S1[i] = add2(S1[i], s[i]); S2[i] = add2(S2[i], q[i]); }
+        float off[S];
+        means_of<VEC, MANY>(S1, cnt, off);
+        squares_of<VEC, MANY>(S2, M2);
+        const float n = (float)(cnt * (MANY ? 1 : VEC));
+#pragma unroll
+        for (int i = 0; i < S; ++i) {
+            mean[i] = shift[i] + off[i];
+            M2[i] = fmaxf(__fmaf_rn(-n * off[i], off[i], M2[i]), 0.f);   // (a NaN: see below)
+            if (off[i] != off[i]) M2[i] = off[i];
+        }
+    }
     ptx::pdl_launch_dependents();
-    block_moments<VEC, MANY>(a, red_mean, red_M2, red_n, gstat);
+    block_moments<VEC, MANY>(a, red_mean, red_M2, red_n, gstat, put_moments<VEC, MANY>(a, mean, M2, (float)cnt, red_mean, red_M2, red_n));
     for (int g = threadIdx.x; g < a.gpb; g += blockDim.x)
-        a.stats[((size_t)img * a.groups + block * a.gpb + g) * a.cluster + piece] = make_float2(gstat[g].mean, gstat[g].M2);
+        a.stats[((size_t)img * a.groups + block * a.gpb + g) * a.cluster + part] = make_float2(gstat[g].mean, gstat[g].M2);
 }
 
 // "twice", the second: the pieces' moments joined, and the values.  Blocks in reverse order: what was read last is in the L2 cache.
 template <int DT, int VEC, bool MANY>
-__global__ void __launch_bounds__(kNormThreads, 4) group_norm_apply_kernel(const NormArgs a)
+__global__ void __launch_bounds__(kNormThreads, 3) group_norm_apply_kernel(const NormArgs a)
 {
-    constexpr int NV = 4;
+    constexpr int S = MANY ? VEC : 1, kPairs = VEC == 1 ? 1 : VEC / 2, NV = kApplyPieces;
+    typedef Piece<DT, VEC> P;
+    extern __shared__ __align__(16) uint8_t hold_bytes[];
     __shared__ float2 fin[kMaxGroups];
-    const int blocks = a.groups / a.gpb;
-    const unsigned id = gridDim.x - 1 - blockIdx.x, unit = id / (unsigned)a.cluster;
-    const int piece = (int)(id - unit * (unsigned)a.cluster);
-    const long long img = unit / (unsigned)blocks;
-    const int block = (int)(unit - (unsigned)img * (unsigned)blocks), c0 = block * a.gpb * a.cpg;
-    const long long p0 = piece * a.span, left = a.P - p0, mine = left < 0 ? 0 : left < a.span ? left : a.span;
-    const size_t row0 = (size_t)img * a.P + p0;
-    const Pieces who(a);
+    const unsigned id = gridDim.x - 1 - blockIdx.x;
+    const long long img = id / (unsigned)a.cluster;
+    const int part = (int)(id - (unsigned)img * (unsigned)a.cluster), block = (int)(gridDim.y - 1 - blockIdx.y), c0 = block * a.gpb * a.cpg;
+    const long long p0 = part * a.span, left = a.P - p0;
+    const int mine = (int)(left < 0 ? 0 : left < a.span ? left : a.span);
+    const Place who(a);
     const int lane = threadIdx.x & 31;
     ptx::pdl_wait();
     for (int g = threadIdx.x >> 5; g < a.gpb; g += (int)blockDim.x >> 5) {
         const float2 *from = a.stats + ((size_t)img * a.groups + block * a.gpb + g) * a.cluster;
-        const float ref = from[0].x;
-        float n[kNormSplits / 32], m[kNormSplits / 32], q[kNormSplits / 32], all = 0.f, d = 0.f, M2 = 0.f;
-#pragma unroll
-        for (int k = 0; k < kNormSplits / 32; ++k) {
-            const int i = lane + 32 * k;
-            n[k] = m[k] = q[k] = 0.f;
-            if (i < a.cluster) {
-                const long long rest = a.P - i * a.span, has = rest < 0 ? 0 : rest < a.span ? rest : a.span;
-                const float2 s = from[i];
-                n[k] = (float)(has * a.cpg);
-                m[k] = s.x;
-                q[k] = s.y;
-            }
-            all += n[k];
-            if (n[k] > 0.f) d = __fmaf_rn(n[k], m[k] - ref, d);
+        float d = 0.f, M2 = 0.f, c = 0.f;
+        const float all = (float)(a.P * a.cpg), each = (float)(a.span * a.cpg);
+        auto weight = [&](int i) {                             // values of piece i
+            const long long rest = a.P - i * a.span;
+            return rest >= a.span ? each : rest > 0 ? (float)(rest * a.cpg) : 0.f;
+        };
+        for (int i = lane; i < a.cluster; i += 32) d = __fmaf_rn(weight(i), from[i].x, d);
+        const float centre = __fdiv_rn(warp_sum(d), all);
+        for (int i = lane; i < a.cluster; i += 32) {
+            const float2 s = from[i];
+            const float w = weight(i), q = s.x - centre, wq = w * q;
+            c += wq;
+            M2 += __fmaf_rn(wq, q, s.y);
         }
-        all = warp_sum(all);
-        const float centre = ref + __fdiv_rn(warp_sum(d), all);
-#pragma unroll
-        for (int k = 0; k < kNormSplits / 32; ++k) { const float o = m[k] - centre; if (n[k] > 0.f) M2 += __fmaf_rn(n[k] * o, o, q[k]); }
         M2 = warp_sum(M2);
-        if (lane == 0) fin[g] = make_float2(centre, deviation_inverse(M2, all, a.eps));
+        c = warp_sum(c);
+        if (lane == 0) fin[g] = make_float2(centre + __fdividef(c, all), deviation_inverse(M2, all, a.eps));
     }
     __syncthreads();
     ptx::pdl_launch_dependents();
-    float2 stat[MANY ? VEC : 1];
+    const int cnt = who.count(a, mine);
+    if (cnt == 0) return;
+    float2 stat[S];
     Affine<VEC, MANY> f;
-    auto column = [&](int c) {
-        column_stats<VEC, MANY>(a, a.cpt > 1 ? 0 : c, fin, stat);
-        f.set(a, c0 + c * VEC, stat);
-    };
+    int ent = 0;
+    column_stats<VEC, MANY>(a, a.cpt > 1 ? 0 : who.col, fin, stat);
+    const size_t e = ((size_t)img * a.P + p0 + who.pl) * a.C + c0 + (size_t)who.col * VEC;
+    const char *from = static_cast<const char *>(a.X) + e * P::kBytes;
+    const int ob = out_bytes(a.out);
     if (a.cpt > 1) {
-        for (long long p = 0; p < mine; ++p)
-            for (int c = who.col; c < a.nch; c += blockDim.x) {
-                Piece<DT, VEC> v;
-                v.load(a.X, (row0 + p) * a.C + c0 + c * VEC);
-                column(c);
-                float x[VEC];
-                v.widen(x);
-                finish_values(a, row0 + p, c0 + c * VEC, x, f);
-            }
+        for (int j = 0; j < cnt; ++j) {
+            const int p = j / who.cols, k = (j - p * who.cols) * (int)blockDim.x, c = c0 + (who.col + k) * VEC;
+            const size_t off = (size_t)p * a.C + (size_t)k * VEC;
+            P v;
+            v.load(from + off * P::kBytes);
+            f.set(a, c, stat);
+            char *to = static_cast<char *>(a.out.Y) + (e + off + slab_shift(a.out, c, &ent)) * ob;
+            pair_t x[1][kPairs];
+            v.widen(x[0]);
+            normalise<VEC, MANY>(x[0], f);
+            store_pieces<VEC, 1>(a, x, [](int) { return true; }, [&](int) { return to; }, [&](int) { return ent; });
+        }
         return;
     }
-    if (!who.live) return;
-    column(who.col);
     const int c = c0 + who.col * VEC;
-    for (long long base = who.pl; base < mine; base += (long long)a.lanes * NV) {
-        Piece<DT, VEC> v[NV];
+    f.set(a, c, stat);
+    char *to = static_cast<char *>(a.out.Y) + (e + slab_shift(a.out, c, &ent)) * ob;
+    const size_t bytes = (size_t)a.lanes * a.C * P::kBytes, far = (size_t)a.lanes * a.C * ob;
+    PieceRing<DT, VEC, NV, kApplyDepth> ring(hold_bytes, from, bytes, cnt);
+    auto batch = [&](auto whole, int n) {                  // (what is not there is not stored)
+        ring.turn();
+        pair_t x[NV][kPairs];
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
-            if (base + j * a.lanes < mine) v[j].load(a.X, (row0 + base + j * a.lanes) * a.C + c);
+        for (int j = 0; j < NV; ++j) ring.piece(j).widen(x[j]);
+        ring.done();
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
-            if (base + j * a.lanes < mine) {
-                float x[VEC];
-                v[j].widen(x);
-                finish_values(a, row0 + base + j * a.lanes, c, x, f);
-            }
-    }
+        for (int j = 0; j < NV; ++j) normalise<VEC, MANY>(x[j], f);
+        store_pieces<VEC, NV>(a, x, [&](int j) { return decltype(whole)::value || j < n; }, [&](int) { char *const here = to; to += far; return here; }, [&](int) { return ent; });
+    };
+    int todo = cnt;
+    for (; todo >= NV; todo -= NV) batch(std::true_type{}, NV);
+    if (todo) batch(std::false_type{}, todo);
 }
 
-// "rows": one position per image.  A warp takes a group at a time (its cpg values are contiguous) and has the next one's values on the way.
+// "rows": one position per image.  A warp takes a group at a time (its cpg values are contiguous) and has the next kRowDepth - 1 on the way, in shared
+// memory of its own; gamma and beta stay in registers where it meets the same channels again (one group, or a stride of whole rows).  NV is the
+// number of a lane's pieces exactly, so that only the last may be missing: with a test on every piece a third of the instructions were branches.
+constexpr int kRowDepth = 4;
 template <int DT, int VEC, int NV>
-__global__ void __launch_bounds__(kNormThreads, NV <= 4 ? 4 : 2) group_norm_rows_kernel(const NormArgs a)
+__global__ void __launch_bounds__(kNormThreads, NV == 1 ? 3 : 2) group_norm_rows_kernel(const NormArgs a)
 {
+    constexpr int kPairs = VEC == 1 ? 1 : VEC / 2, kSlot = NV * 32 * (VEC == 1 ? 4 : 16);
+    constexpr bool kKeep = NV * VEC <= 24;
+    typedef Piece<DT, VEC> P;
+    extern __shared__ __align__(16) uint8_t hold_bytes[];
     const int lane = threadIdx.x & 31;
-    const long long total = a.Nb * a.groups, step = (long long)gridDim.x * (blockDim.x >> 5);
-    long long seg = (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
+    const int total = (int)(a.Nb * a.groups), step = (int)(gridDim.x * (blockDim.x >> 5));   // (the host takes no more than 2^31 of them)
+    int seg = (int)(blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5));
+    const bool last = lane + 32 * (NV - 1) < a.nch;
     ptx::pdl_wait();
-    Piece<DT, VEC> next[NV], v[NV];
-    auto request = [&](long long s) {
+    if (seg >= total) return;
+    // [group of the warp][piece][lane]
+    uint8_t *const hold = hold_bytes + (threadIdx.x >> 5) * (kRowDepth * kSlot) + lane * (VEC == 1 ? 4 : 16);
+    const char *from = static_cast<const char *>(a.X) + ((size_t)seg * a.cpg + lane * VEC) * P::kBytes;
+    const size_t stride = (size_t)step * a.cpg * P::kBytes;
+    auto request = [&](bool there, int slot) {             // (an empty batch of copies where there is no such group)
+        if (there) {
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
-            if (lane + 32 * j < a.nch) next[j].load(a.X, (size_t)s * a.cpg + (lane + 32 * j) * VEC);
+            for (int j = 0; j < NV; ++j)
+                if (j < NV - 1 || last) {
+                    uint8_t *const to = hold + slot + j * 32 * (VEC == 1 ? 4 : 16);
+                    if constexpr (VEC == 1) {
+                        P v;
+                        v.load(from + j * 32 * VEC * P::kBytes);
+                        *reinterpret_cast<float *>(to) = v.raw;
+                    } else {
+                        ptx::cp_async_16(ptx::smem_u32(to), from + j * 32 * VEC * P::kBytes);
+                    }
+                }
+        }
+        ptx::cp_async_commit();
+        from += stride;
     };
-    if (seg < total) request(seg);
-    for (; seg < total; seg += step) {
+    int ahead = seg, slot = 0;
 #pragma unroll
-        for (int j = 0; j < NV; ++j) v[j] = next[j];
-        if (seg + step < total) request(seg + step);
-        else ptx::pdl_launch_dependents();
-        float s = 0.f;
+    for (int k = 0; k < kRowDepth - 1; ++k, ahead = ahead < total - step ? ahead + step : total) request(ahead < total, k * kSlot);
+    pair_t gamma[kKeep ? NV : 1][kPairs], beta[kKeep ? NV : 1][kPairs];
+    int shift[NV], ent[NV], held = -1;
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
-            if (lane + 32 * j < a.nch) {
-                float x[VEC];
-                v[j].widen(x);
-#pragma unroll
-                for (int w = VEC / 2; w; w >>= 1)
-#pragma unroll
-                    for (int i = 0; i < w; ++i) x[i] += x[i + w];
-                s += x[0];
-            }
-        const float mean = __fdiv_rn(warp_sum(s), (float)a.cpg);
-        float q = 0.f;
+    for (int j = 0; j < NV; ++j) shift[j] = ent[j] = 0;
+    const int ob = out_bytes(a.out), next_piece = 32 * VEC * ob;
+    char *to = static_cast<char *>(a.out.Y) + ((size_t)seg * a.cpg + lane * VEC) * ob;
+    const size_t far = (size_t)step * a.cpg * ob;
+    const float count = (float)a.cpg, inverse = __frcp_rn(count);
+    for (;;) {
+        request(ahead < total, slot == 0 ? (kRowDepth - 1) * kSlot : slot - kSlot);
+        if (ahead < total) ahead = ahead < total - step ? ahead + step : total;
+        ptx::cp_async_wait_but<kRowDepth - 1>();           // (each lane reads what it asked for itself)
+        pair_t x[NV][kPairs], s[kPairs];
 #pragma unroll
         for (int j = 0; j < NV; ++j)
-            if (lane + 32 * j < a.nch) {
-                float x[VEC];
-                v[j].widen(x);
+            if (j < NV - 1 || last) {
+                P v;
+                v.raw = *reinterpret_cast<const typename P::Raw *>(hold + slot + j * 32 * (VEC == 1 ? 4 : 16));
+                v.widen(x[j]);
+            } else {
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) { const float d = x[i] - mean; q = __fmaf_rn(d, d, q); }
+                for (int i = 0; i < kPairs; ++i) x[j][i] = pair(0.f, 0.f);
             }
-        const float rstd = deviation_inverse(warp_sum(q), (float)a.cpg, a.eps);
-        const long long row = a.groups == 1 ? seg : seg / a.groups;
-        const int c0 = a.groups == 1 ? 0 : (int)(seg - row * a.groups) * a.cpg;
-        const float2 stat = make_float2(mean, rstd);
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
-            if (lane + 32 * j < a.nch) {
-                const int c = c0 + (lane + 32 * j) * VEC;
-                float x[VEC];
-                Affine<VEC, false> f;
-                v[j].widen(x);
-                f.set(a, c, &stat);
-                finish_values(a, (size_t)row, c, x, f);
+        for (int i = 0; i < kPairs; ++i) {
+            s[i] = x[0][i];
+#pragma unroll
+            for (int j = 1; j < NV; ++j) s[i] = add2(s[i], x[j][i]);
+        }
+        slot = slot == (kRowDepth - 1) * kSlot ? 0 : slot + kSlot;
+        const float mean = divide(warp_sum(fold<kPairs>(s)), count, inverse);
+        const pair_t minus = pair(-mean, VEC == 1 ? 0.f : -mean), minus_last = last ? minus : pair(0.f, 0.f);
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                x[j][i] = add2(x[j][i], j < NV - 1 ? minus : minus_last);
+                s[i] = j == 0 ? mul2(x[j][i], x[j][i]) : fma2(x[j][i], x[j][i], s[i]);
             }
+        }
+        const int g = a.groups == 1 ? 0 : seg % a.groups;
+        if (g != held) {
+            held = g;
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+                if (j < NV - 1 || last) {
+                    const int c = g * a.cpg + (lane + 32 * j) * VEC;
+                    if (kKeep) load_affine<VEC>(a, c, gamma[kKeep ? j : 0], beta[kKeep ? j : 0]);
+                    shift[j] = slab_shift(a.out, c, &ent[j]);
+                }
+        }
+        const float rstd = deviation_inverse(warp_sum(fold<kPairs>(s)), count, a.eps);
+        const pair_t r = pair(rstd, rstd);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            if (!kKeep && (j < NV - 1 || last)) load_affine<VEC>(a, g * a.cpg + (lane + 32 * j) * VEC, gamma[0], beta[0]);
+#pragma unroll
+            for (int i = 0; i < kPairs; ++i) x[j][i] = fma2(x[j][i], mul2(gamma[kKeep ? j : 0][i], r), beta[kKeep ? j : 0][i]);
+        }
+        store_pieces<VEC, NV>(a, x, [&](int j) { return j < NV - 1 || last; }, [&](int j) { return to + (j * next_piece + shift[j]); }, [&](int j) { return ent[j]; });
+        if (seg >= total - step) break;
+        seg += step;
+        to += far;
     }
+    ptx::pdl_launch_dependents();
 }
 
 // ------------------------------------------------------------------------------------ host side
-template <int DT, int VEC, int NV, bool MANY> static int launch_held(const NormArgs &a, const NormPlan &p, cudaStream_t st)
+// Dynamic shared memory beyond the default, once per kernel and device whatever the size asked for later.
+template <class K> static int allow_smem(K kernel, bool (&done)[64], int bytes)
 {
+    int dev = 0;
+    cudaGetDevice(&dev);
+    if (dev < 64 && done[dev]) return FLEXIQ_OK;
+    FLEXIQ_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+    if (dev < 64) done[dev] = true;
+    return FLEXIQ_OK;
+}
+template <int DT, int VEC, bool MANY, int T> static int launch_held_threads(const NormArgs &a, const NormPlan &p, cudaStream_t st)
+{
+    static bool done[64] = {};
+    if (int rc = allow_smem(group_norm_held_kernel<DT, VEC, MANY, T>, done, kNormHold)) return rc;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(a.Nb * (a.groups / a.gpb) * a.cluster), 1, 1);
-    cfg.blockDim = dim3((unsigned)p.threads, 1, 1);
+    cfg.gridDim = dim3((unsigned)(a.Nb << a.cluster_log), (unsigned)(a.groups / a.gpb), 1);
+    cfg.blockDim = dim3((unsigned)T, 1, 1);
+    cfg.dynamicSmemBytes = (size_t)p.nv * T * (VEC == 1 ? 4 : 16);
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = (unsigned)a.cluster;
+    attr[1].val.clusterDim.x = 1u << a.cluster_log;
     attr[1].val.clusterDim.y = 1;
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = a.cluster > 1 ? 2 : 1;
-    FLEXIQ_CUDA_TRY(cudaLaunchKernelEx(&cfg, group_norm_held_kernel<DT, VEC, NV, MANY>, a));
+    cfg.numAttrs = a.cluster_log ? 2 : 1;
+    FLEXIQ_CUDA_TRY(cudaLaunchKernelEx(&cfg, group_norm_held_kernel<DT, VEC, MANY, T>, a));
     return FLEXIQ_OK;
 }
-template <int DT, int VEC, bool MANY> static int launch_held_nv(const NormArgs &a, const NormPlan &p, cudaStream_t st)
+template <int DT, int VEC, bool MANY> static int launch_held(const NormArgs &a, const NormPlan &p, cudaStream_t st)
 {
-    switch (p.nv) {
-        case 1: return launch_held<DT, VEC, 1, MANY>(a, p, st);
-        case 2: return launch_held<DT, VEC, 2, MANY>(a, p, st);
-        case 4: return launch_held<DT, VEC, 4, MANY>(a, p, st);
-        case 8: return launch_held<DT, VEC, 8, MANY>(a, p, st);
-        default: return launch_held<DT, VEC, 16, MANY>(a, p, st);
+    switch (p.threads) {
+        case 64: return launch_held_threads<DT, VEC, MANY, 64>(a, p, st);
+        case 128: return launch_held_threads<DT, VEC, MANY, 128>(a, p, st);
+        case 256: return launch_held_threads<DT, VEC, MANY, 256>(a, p, st);
+        default: return launch_held_threads<DT, VEC, MANY, 512>(a, p, st);
     }
 }
 template <int DT, int VEC, bool MANY> static int launch_twice(const NormArgs &a, const NormPlan &p, cudaStream_t st)
 {
-    const unsigned grid = (unsigned)(a.Nb * (a.groups / a.gpb) * a.cluster);
-    FLEXIQ_CUDA_TRY(launch_pdl(group_norm_stats_kernel<DT, VEC, MANY>, grid, (unsigned)p.threads, 0, st, a));
-    FLEXIQ_CUDA_TRY(launch_pdl(group_norm_apply_kernel<DT, VEC, MANY>, grid, (unsigned)p.threads, 0, st, a));
+    const dim3 grid((unsigned)(a.Nb * a.cluster), (unsigned)(a.groups / a.gpb), 1);
+    constexpr int kStats = kNormThreads * kStatsPieces * kStatsDepth * (VEC == 1 ? 4 : 16), kApply = kNormThreads * kApplyPieces * kApplyDepth * (VEC == 1 ? 4 : 16);
+    static bool done[2][64] = {};
+    if (int rc = allow_smem(group_norm_stats_kernel<DT, VEC, MANY>, done[0], kStats)) return rc;
+    if (int rc = allow_smem(group_norm_apply_kernel<DT, VEC, MANY>, done[1], kApply)) return rc;
+    FLEXIQ_CUDA_TRY(launch_pdl(group_norm_stats_kernel<DT, VEC, MANY>, grid, (unsigned)p.threads, kStats, st, a));
+    FLEXIQ_CUDA_TRY(launch_pdl(group_norm_apply_kernel<DT, VEC, MANY>, grid, (unsigned)p.threads, kApply, st, a));
+    return FLEXIQ_OK;
+}
+template <int DT, int VEC, int NV> static int launch_rows_nv(const NormArgs &a, int sms, cudaStream_t st)
+{
+    // few rows: as many blocks as there are; many: as many blocks of eight warps as an SM holds, each warp walking over rows
+    const long long total = a.Nb * a.groups;
+    const unsigned threads = total < 8ll * sms ? 64 : kNormThreads;
+    long long blocks = ceil_div(total, threads / 32);
+    const long long most = (NV == 1 ? 3ll : 2ll) * sms;
+    if (blocks > most && threads == kNormThreads) blocks = most;
+    constexpr int kRow = kRowDepth * NV * (VEC == 1 ? 4 : 16);   // a thread's slots
+    static bool done[64] = {};
+    if (int rc = allow_smem(group_norm_rows_kernel<DT, VEC, NV>, done, kNormThreads * kRow)) return rc;
+    FLEXIQ_CUDA_TRY(launch_pdl(group_norm_rows_kernel<DT, VEC, NV>, (unsigned)blocks, threads, (size_t)threads * kRow, st, a));
     return FLEXIQ_OK;
 }
 template <int DT, int VEC> static int launch_norm_rows(const NormArgs &a, const NormPlan &p, int sms, cudaStream_t st)
 {
-    // few rows: as many blocks as there are; many: four blocks of eight warps an SM, each walking over rows
-    const long long total = a.Nb * a.groups;
-    const unsigned threads = total < 8ll * sms ? 64 : kNormThreads;
-    long long blocks = ceil_div(total, threads / 32);
-    const long long most = 4ll * sms;
-    if (blocks > most && threads == kNormThreads) blocks = most;
-    auto go = [&](auto kernel) -> int { FLEXIQ_CUDA_TRY(launch_pdl(kernel, (unsigned)blocks, threads, 0, st, a)); return FLEXIQ_OK; };
     switch (p.nv) {
-        case 1: return go(group_norm_rows_kernel<DT, VEC, 1>);
-        case 2: return go(group_norm_rows_kernel<DT, VEC, 2>);
-        case 3: return go(group_norm_rows_kernel<DT, VEC, 3>);
-        case 4: return go(group_norm_rows_kernel<DT, VEC, 4>);
-        case 5: case 6: return go(group_norm_rows_kernel<DT, VEC, 6>);
-        default: return go(group_norm_rows_kernel<DT, VEC, 8>);
+        case 1: return launch_rows_nv<DT, VEC, 1>(a, sms, st);
+        case 2: return launch_rows_nv<DT, VEC, 2>(a, sms, st);
+        case 3: return launch_rows_nv<DT, VEC, 3>(a, sms, st);
+        case 4: return launch_rows_nv<DT, VEC, 4>(a, sms, st);
+        case 5: return launch_rows_nv<DT, VEC, 5>(a, sms, st);
+        case 6: return launch_rows_nv<DT, VEC, 6>(a, sms, st);
+        case 7: return launch_rows_nv<DT, VEC, 7>(a, sms, st);
+        default: return launch_rows_nv<DT, VEC, 8>(a, sms, st);
     }
 }
 template <int DT> static int launch_norm(const NormArgs &a, const NormPlan &p, int sms, cudaStream_t st)
 {
     constexpr int V = FullVec<DT>::v;
     if (p.kind == kNormRows) return p.vec == 1 ? launch_norm_rows<DT, 1>(a, p, sms, st) : launch_norm_rows<DT, V>(a, p, sms, st);
-    if (p.kind == kNormHeld) return p.vec == 1 ? launch_held_nv<DT, 1, false>(a, p, st) : p.many ? launch_held_nv<DT, V, true>(a, p, st) : launch_held_nv<DT, V, false>(a, p, st);
+    if (p.kind == kNormHeld) return p.vec == 1 ? launch_held<DT, 1, false>(a, p, st) : p.many ? launch_held<DT, V, true>(a, p, st) : launch_held<DT, V, false>(a, p, st);
     return p.vec == 1 ? launch_twice<DT, 1, false>(a, p, st) : p.many ? launch_twice<DT, V, true>(a, p, st) : launch_twice<DT, V, false>(a, p, st);
+}
+
+unsigned norm_status()
+{
+    unsigned word = 0;
+    const unsigned zero = 0;
+    if (cudaMemcpyFromSymbol(&word, g_norm_status, sizeof(word)) != cudaSuccess) return 0;   // the caller's own read reports it
+    if (word) cudaMemcpyToSymbol(g_norm_status, &zero, sizeof(zero));
+    return word;
 }
 
 static int check_shape(int x_dtype, int64_t Nb, int64_t P, int C, int groups)
@@ -710,13 +1047,18 @@ static int run_norm(NormArgs &a, int x_dtype, void *scratch, cudaStream_t st)
 {
     const int sms = plan_sms();
     const NormPlan p = plan_norm(x_dtype, a.Nb, a.P, a.C, a.groups, sms);
-    if (p.kind != kNormRows && a.Nb * (a.groups / p.gpb) * (long long)p.cluster > 0x7fffffffll)
+    if ((p.kind == kNormRows ? a.Nb * a.groups : a.Nb * (long long)p.cluster) > 0x40000000ll || (p.kind != kNormRows && a.groups / p.gpb > 65535))
         return set_error(FLEXIQ_ERR_UNSUPPORTED, "too many images and groups for one launch");
     if (p.kind == kNormTwice && (!scratch || (reinterpret_cast<uintptr_t>(scratch) & 15)))
         return set_error(FLEXIQ_ERR_INVALID_ARG, "scratch_dev is NULL or not 16-byte aligned: this shape needs %lld bytes", scratch_bytes(p, a.Nb, a.groups));
     a.cpg = a.C / a.groups;
     a.gpb = p.gpb; a.nch = p.nch; a.cpt = p.cpt; a.lanes = p.lanes; a.cluster = p.cluster; a.span = p.span;
     a.stats = static_cast<float2 *>(scratch);
+    for (a.cluster_log = 0; (1 << a.cluster_log) < p.cluster; ++a.cluster_log) {}
+    auto inverse = [](int d) { return d > 1 ? (unsigned)((0x100000000ull + d - 1) / d) : 0u; };   // (exact for numerators below 2^16 and such d)
+    const int sub = p.many && p.vec % a.cpg == 0 && a.cpg > 1 ? p.vec / a.cpg : p.many ? p.vec : 1;
+    const int each = p.cpt > 1 ? kNormThreads : p.many ? (sub < p.vec ? 1 : a.cpg) : a.cpg / p.vec;
+    a.by_nch = inverse(p.nch); a.by_lanes = inverse(p.lanes); a.by_cpg = inverse(a.cpg); a.by_each = inverse(each);
     switch (x_dtype) {
         case FLEXIQ_DTYPE_F32: return launch_norm<FLEXIQ_DTYPE_F32>(a, p, sms, st);
         case FLEXIQ_DTYPE_F16: return launch_norm<FLEXIQ_DTYPE_F16>(a, p, sms, st);

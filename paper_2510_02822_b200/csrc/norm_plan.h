@@ -5,8 +5,9 @@
 namespace flexiq {
 
 constexpr int kNormThreads = 256;
+constexpr int kNormHold = 65536;        // bytes a block holds ("held")
 constexpr int kNormCluster = 8;        // blocks of a cluster at most ("held")
-constexpr int kNormSplits = 64;        // pieces of an image's channel block at most ("twice")
+constexpr int kNormSplits = 256;       // pieces of an image's channel block at most ("twice")
 constexpr int kMaxGroups = 128;        // groups of a channel block at most
 
 enum NormKind { kNormRows, kNormHeld, kNormTwice };
@@ -47,11 +48,11 @@ inline NormPlan plan_norm(int x_dtype, long long Nb, long long P, int C, int gro
         if ((long long)unit_groups * next * cpg / p.vec > kNormThreads || unit_groups * next > kMaxGroups) break;
         m = next;
     }
-    constexpr int kMaxNv = 16;
     for (int w = m; w >= 1; --w) {
         if (units % w) continue;
         shape(w);
-        const long long capacity = p.cpt > 1 ? kMaxNv / p.cpt : (long long)(kNormThreads / p.nch) * kMaxNv;   // positions a block holds
+        // positions a block holds: 64 KB of pieces (two blocks an SM), eight a thread of 512 (a piece of the scalar form is shorter, but as long to work on)
+        const long long capacity = p.cpt > 1 ? 16 / p.cpt : (long long)(512 / p.nch) * 8;
         if (capacity < 1 || ceil_div(P, capacity) > kNormCluster) continue;
         p.kind = kNormHeld;
         p.threads = kNormThreads;
@@ -62,22 +63,32 @@ inline NormPlan plan_norm(int x_dtype, long long Nb, long long P, int C, int gro
         p.cluster = k;
         p.span = ceil_div(P, k);
         if (p.cpt == 1) {
+            // threads for about four pieces each: the passes over them are a chain of latencies.  Where there are blocks for every SM a thread's fixed
+            // work counts as well, and 256 do
+            while (p.threads < 512 && (blocks * k < sms || ceil_div(p.span, p.threads / p.nch) > 16) && ceil_div(p.span, p.threads / p.nch) > 6) p.threads *= 2;
             while (p.threads > 64 && p.threads / 2 >= p.nch && ceil_div(p.span, p.threads / 2 / p.nch) <= 4) p.threads /= 2;
             p.lanes = p.threads / p.nch;
-            p.nv = round_up_pow2(ceil_div(p.span, p.lanes));
+            p.nv = (int)ceil_div(p.span, p.lanes);
         } else {
             p.lanes = 1;
-            p.nv = round_up_pow2(p.span * p.cpt);
+            p.nv = (int)(p.span * p.cpt);
         }
         return p;
     }
+    // nothing to be held: as much of a position as a block's threads take, up to 1 KB, which is read in longer runs
+    for (int w = units; w > m; --w)
+        if (units % w == 0 && unit_groups * w <= kMaxGroups && (long long)unit_groups * w * cpg * bytes <= 1024 && (long long)unit_groups * w * cpg / p.vec <= kNormThreads) { m = w; break; }
     shape(m);
     p.kind = kNormTwice;
     p.threads = kNormThreads;
     p.lanes = p.cpt > 1 ? 1 : kNormThreads / p.nch;
-    // pieces: some four blocks an SM, and at least a few steps each
-    const long long blocks = Nb * (units / m), steps = p.cpt > 1 ? P : ceil_div(P, (long long)p.lanes * 8);
-    long long k = ceil_div(4ll * sms, blocks);
+    // pieces: as many as make whole waves of two blocks an SM (nine tenths of one at least, where up to four waves allow that), and a few steps each
+    const long long blocks = Nb * (units / m), steps = p.cpt > 1 ? P : ceil_div(P, (long long)p.lanes * 8), wave = 2ll * sms;
+    long long k = 1;
+    for (long long w = 1; w <= 4; ++w) {
+        k = w * wave / blocks;
+        if (k * blocks * 10 >= w * wave * 9) break;
+    }
     if (k > steps) k = steps;
     if (k > kNormSplits) k = kNormSplits;
     p.cluster = (int)(k < 1 ? 1 : k);

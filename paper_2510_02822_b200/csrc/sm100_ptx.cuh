@@ -313,6 +313,15 @@ __device__ __forceinline__ void mma_commit_s(uint32_t bar)
         asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 
+// ---- asynchronous copies of 16 bytes into shared memory; a thread waits for its own --------
+__device__ __forceinline__ void cp_async_16(uint32_t dst, const void *src)
+{
+    asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_async_wait_but() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }   // all but the last N batches
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
 // ---- thread-block clusters and CTA pairs (cta_group::2) ------------------------------
 __device__ __forceinline__ uint32_t cluster_ctarank()
 {
@@ -351,6 +360,11 @@ __device__ __forceinline__ void mbar_arrive_cluster_relaxed(uint32_t cluster_add
 __device__ __forceinline__ void cluster_sync_all()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// Eight bytes into the shared memory of a CTA of the cluster, credited to an mbarrier there (both addresses from mapa)
+__device__ __forceinline__ void st_async_64(uint32_t cluster_addr, float a, float b, uint32_t mbar_cluster_addr)
+{
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(cluster_addr), "f"(a), "f"(b), "r"(mbar_cluster_addr) : "memory");
 }
 // The same in two halves: what lies between them may not touch the other CTAs' memory.
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }

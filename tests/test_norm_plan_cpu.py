@@ -10,6 +10,7 @@ SRC = r"""
 #include <random>
 #include <vector>
 using namespace flexiq;
+static unsigned r0 = 0;
 static int fail(const char *what, int dt, long long Nb, long long P, int C, int g) { printf("%s: type %d, %lld x %lld x %d, %d groups\n", what, dt, Nb, P, C, g); return 1; }
 static int check(int dt, long long Nb, long long P, int C, int groups)
 {
@@ -23,13 +24,13 @@ static int check(int dt, long long Nb, long long P, int C, int groups)
     }
     if (p.gpb < 1 || groups % p.gpb || p.gpb > kMaxGroups || p.nch * p.vec != p.gpb * cpg) return bad("channel block");
     if (p.vec > 1 && (p.gpb * cpg) % p.vec) return bad("pieces that leave the block");
-    if (p.threads > kNormThreads || p.threads % 32 || p.threads < 32) return bad("threads");
+    if (p.threads > 512 || (p.kind == kNormTwice && p.threads != kNormThreads) || p.threads % 32 || p.threads < 32) return bad("threads");
     if (!p.many && cpg % p.vec) return bad("a piece of two groups summed as one");
     if (p.cpt > 1 && (p.gpb != 1 || p.many || p.threads != kNormThreads || p.lanes != 1 || p.cpt * p.threads < p.nch)) return bad("wide positions");
     if (p.cpt == 1 && (p.lanes < 1 || p.lanes * p.nch > p.threads)) return bad("lanes");
     if (p.cluster < 1 || p.cluster > (p.kind == kNormHeld ? kNormCluster : kNormSplits) || p.span * p.cluster < P || p.span < 1) return bad("pieces of an image");
     if (p.kind == kNormHeld) {
-        if ((p.cluster & (p.cluster - 1)) || (p.nv & (p.nv - 1)) || p.nv < 1 || p.nv > 16) return bad("powers of two");
+        if ((p.cluster & (p.cluster - 1)) || p.nv < 1 || p.nv * p.threads * 16 > kNormHold || (p.threads != 64 && p.threads != 128 && p.threads != 256 && p.threads != 512)) return bad("what a block holds");
         std::vector<unsigned char> seen((size_t)p.span * p.nch, 0);
         for (int t = 0; t < p.threads; ++t) {
             int pl, col, k = 0;
@@ -43,6 +44,13 @@ static int check(int dt, long long Nb, long long P, int C, int groups)
         }
         for (unsigned char s : seen) if (s != 1) return bad("not held");
     }
+    auto inverse = [](int d) { return d > 1 ? (unsigned)((0x100000000ull + d - 1) / d) : 0u; };
+    for (int d : {p.nch, p.lanes, cpg}) {
+        const unsigned inv = inverse(d);
+        for (int n = (int)(r0 % 97); n < 65536; n += 61)
+            if ((inv ? (int)(((unsigned long long)n * inv) >> 32) : n) != n / d) return bad("quotients by multiplication");
+    }
+    ++r0;
     const int S = p.many ? p.vec : 1, pitch = p.cpt > 1 ? p.threads : p.nch * S, each = p.cpt > 1 ? p.threads : (p.many ? cpg : cpg / p.vec);
     if ((p.lanes - 1) * pitch + p.gpb * each > p.threads * S) return bad("entries");
     return 0;
