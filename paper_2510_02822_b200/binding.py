@@ -377,6 +377,16 @@ def _check_tensor(t, what, numel, device, dtypes):
             f"{what} must be a contiguous tensor of {numel} elements on {device}, of type {' or '.join(str(d) for d in dtypes)}")
 
 
+_FLOAT_CODES = {}
+
+
+def _float_code(dtype):
+    if not _FLOAT_CODES:
+        import torch
+        _FLOAT_CODES.update({torch.float32: DTYPE_F32, torch.float16: DTYPE_F16, torch.bfloat16: DTYPE_BF16})
+    return _FLOAT_CODES.get(dtype)
+
+
 def _float_types():
     import torch
     return torch.float32, torch.float16, torch.bfloat16
@@ -411,17 +421,16 @@ def _norm_scratch(X, Nb, P, C_, groups):
 def group_norm(X, groups, gamma=None, beta=None, eps=1e-5, act=ACT_NONE, out_dtype=None, Y=None):
     """act((X - mean) / sqrt(var + eps) * gamma + beta) of a channels-last tensor [images, ..., channels], mean and variance per image and
     group of channels (flexiq_group_norm).  groups = 1 on a [rows, channels] tensor is layer normalisation.  out_dtype: X's by default."""
-    import torch
     native = _native_calls()
-    codes = {torch.float32: DTYPE_F32, torch.float16: DTYPE_F16, torch.bfloat16: DTYPE_BF16}
     if out_dtype is None:
         out_dtype = X.dtype if Y is None else Y.dtype
-    code = codes.get(out_dtype)
+    code = _float_code(out_dtype)
     _refuse(code is not None, f"out_dtype {out_dtype} is not float32, float16 or bfloat16")
     if native is not None:
         r = native.group_norm(X, groups, gamma, beta, eps, act, code, Y)
         if r is not NotImplemented:
             return r
+    import torch
     Nb, P, channels = _norm_args(X, gamma, beta)
     if Y is None:
         Y = torch.empty(X.shape, dtype=out_dtype, device=X.device)

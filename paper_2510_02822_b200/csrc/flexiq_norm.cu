@@ -3,7 +3,7 @@
 //   y = act((x - mean) / sqrt(var + eps) * gamma[c] + beta[c]),   mean and var over an image's positions and a group's channels
 //
 // Bound by memory: every input byte is to be read once and every output byte written once.  Three ways, by what fits where:
-//   rows   one position per image (layer normalisation): a warp holds a group in registers
+//   rows   one position per image (layer normalisation): a warp, or four, holds a group in registers
 //   held   an image's block of channels (whole groups, 128 bytes a position where that is enough) is held in the shared memory of a block, or of a
 //          cluster of up to eight, between the statistics and their use; the blocks of a cluster exchange their groups' statistics
 //          through distributed shared memory
@@ -53,9 +53,12 @@ struct NormArgs {
     int cpt;                  // pieces of a position a thread has where there are more than threads, else 1
     int lanes;                // positions side by side in a block
     int cluster;              // blocks per image and channel block ("held"), or pieces of the image ("twice")
-    int cluster_log;          // "held": its logarithm
+    int cluster_log;          // "held": its logarithm; "twice": that of the blocks whose statistics are joined in a cluster
+    int joined;               // "twice": what that leaves of each image
     long long span;           // positions of one of them
-    unsigned by_nch, by_lanes, by_cpg, by_each;   // 2^32 / those, rounded up: quotients of less than 2^16 by a multiplication
+    unsigned by_nch, by_lanes, by_cpg;   // 2^32 / those, rounded up: quotients of less than 2^16 by a multiplication
+    int cuts;                 // "twice": the second kernel's own pieces, and positions of one
+    long long cut_span;
     float2 *stats;            // "twice": [image][group][piece] mean, M2
 };
 
@@ -295,85 +298,88 @@ template <int VEC, bool MANY> __device__ __forceinline__ void squares_of(const p
 
 __device__ unsigned int g_norm_status = 0;
 
-// What the threads of a block found -> their groups' moments in gstat[0 .. gpb): some lanes per group over its threads' entries.  MANY: a thread has `sub`
-// entries, one for each group its piece holds where those are whole, else one for each channel.
-template <int VEC, bool MANY>
-__device__ __forceinline__ void block_moments(const NormArgs &a, const float *red_mean, const float *red_M2, const float *red_n, Moments *gstat, int sub_entries)
+// A thread's moments as entries, [entry][thread], and its number of pieces.  One, where a piece's channels are of one group; MANY: one for each of the groups it has a part of, in order,
+// from the channels' own (K the first one's mean, s and ss the sums of the others' distances from it and of their squares).
+template <int VEC, bool MANY, int T>
+__device__ __forceinline__ void put_moments(const NormArgs &a, int col, const float *mean, const float *M2, float pieces, float *red_mean, float *red_M2, float *red_n)
+{
+    const int t = threadIdx.x;
+    red_n[t] = pieces;
+    if (!MANY) {
+        red_mean[t] = mean[0];
+        red_M2[t] = M2[0];
+        return;
+    }
+    int left = a.cpg - (col * VEC - quotient(col * VEC, a.by_cpg) * a.cpg), at = t;
+    float K = mean[0], s = 0.f, ss = 0.f, M = 0.f, c = 0.f;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+        const float d = mean[i] - K;
+        s += d;
+        ss = __fmaf_rn(d, d, ss);
+        M += M2[i];
+        c += 1.f;
+        if (--left == 0 || i == VEC - 1) {
+            const float away = __fdividef(s, c);
+            red_mean[at] = K + away;
+            red_M2[at] = pieces > 0.f ? __fmaf_rn(pieces, fmaxf(__fmaf_rn(-s, away, ss), 0.f), M) : 0.f;
+            at += T;
+            left = a.cpg;
+            if (i + 1 < VEC) { K = mean[(i + 1) % VEC]; s = ss = M = c = 0.f; }
+        }
+    }
+}
+// The threads' entries -> their groups' moments in gstat[0 .. gpb): some lanes per group over the columns that hold a part of it, at every position.
+template <int VEC, bool MANY, int T>
+__device__ __forceinline__ void block_moments(const NormArgs &a, const float *red_mean, const float *red_M2, const float *red_n, Moments *gstat)
 {
     __syncthreads();
-    const int warps = blockDim.x >> 5;
-    int width = 32;                                   // lanes per group: fewer where there are more groups than warps
-    while (width > 4 && warps * (32 / width) < a.gpb) width >>= 1;
-    const int sub = threadIdx.x & (width - 1), step = blockDim.x >> (31 - __clz(width)), sub_log = 31 - __clz(sub_entries);
-    // entries of a position, and of a group among them
-    const int pitch = a.cpt > 1 ? (int)blockDim.x : a.nch * sub_entries, each = a.cpt > 1 ? (int)blockDim.x : MANY ? (sub_entries < VEC ? 1 : a.cpg) : a.cpg / VEC;
-    const int jump = quotient(width, a.by_each), rest = width - jump * each, row0 = quotient(sub, a.by_each), in0 = sub - row0 * each;
+    int width_log = 5;                                // lanes per group: fewer where there are more groups than warps
+    while (width_log > 2 && (T >> width_log) < a.gpb) --width_log;
+    const int width = 1 << width_log, sub = threadIdx.x & (width - 1), step = T >> width_log;
+    const int pitch = a.cpt > 1 ? T : a.nch;          // threads of a position
     for (int g0 = 0; g0 < a.gpb; g0 += step) {        // (all lanes stay: the sums need them)
-        const int g = g0 + (int)(threadIdx.x >> (31 - __clz(width)));
-        const int rows = g < a.gpb ? a.lanes : 0, first = g < a.gpb ? g * each : 0;
+        const int g = g0 + (int)(threadIdx.x >> width_log);
+        const bool live = g < a.gpb;
+        int col0 = 0, cols;                           // its columns
+        if (a.cpt > 1) cols = T;
+        else if (!MANY) { cols = a.cpg / VEC; col0 = g * cols; }
+        else { col0 = g * a.cpg / VEC; cols = ((g + 1) * a.cpg - 1) / VEC - col0 + 1; }
+        // the lane's entries: (position row, column in), `width` further each time
+        const unsigned by_cols = cols > 1 ? 0xffffffffu / (unsigned)cols + 1u : 0u;
+        const int jump = quotient(width, by_cols), rest = width - jump * cols, row0 = quotient(sub, by_cols), in0 = sub - row0 * cols, rows = live ? a.lanes : 0;
         auto over = [&](auto take) {
             for (int row = row0, in = in0; row < rows;) {
-                const int e = row * pitch + first + in;
-                take(MANY ? red_n[e >> sub_log] : red_n[e], e);
+                const int col = col0 + in, t = row * pitch + col;
+                if (MANY) {                               // the entry, and how many of the piece's channels it has
+                    const int c0 = col * VEC, lo = g * a.cpg, from = c0 > lo ? c0 : lo, to = c0 + VEC < lo + a.cpg ? c0 + VEC : lo + a.cpg;
+                    take(t + (g - quotient(c0, a.by_cpg)) * T, red_n[t] * (float)(to - from));
+                } else {
+                    take(t, red_n[t] * (float)VEC);
+                }
                 row += jump;
                 in += rest;
-                if (in >= each) { in -= each; ++row; }
+                if (in >= cols) { in -= cols; ++row; }
             }
         };
         float n = 0.f, d = 0.f, M2 = 0.f, c = 0.f;
-        over([&](float w, int e) {
+        over([&](int e, float w) {
             n += w;
             d = __fmaf_rn(w, red_mean[e], d);
         });
         n = part_sum(n, width);
         d = part_sum(d, width);
         const float mean = n > 0.f ? __fdiv_rn(d, n) : 0.f;
-        over([&](float w, int e) {
+        over([&](int e, float w) {
             const float q = red_mean[e] - mean, wq = w * q;
             c += wq;
             M2 += __fmaf_rn(wq, q, red_M2[e]);             // (a thread without values: all zero)
         });
         M2 = part_sum(M2, width);
         c = part_sum(c, width);
-        if (sub == 0 && g < a.gpb) gstat[g] = Moments{n, n > 0.f ? mean + __fdividef(c, n) : 0.f, M2};
+        if (sub == 0 && live) gstat[g] = Moments{n, n > 0.f ? mean + __fdividef(c, n) : 0.f, M2};
     }
     __syncthreads();
-}
-// A thread's moments to its entries (the array's size: kNormThreads * VEC for MANY).  Returns the entries of a thread.
-template <int VEC, bool MANY>
-__device__ __forceinline__ int put_moments(const NormArgs &a, const float *mean, const float *M2, float pieces, float *red_mean, float *red_M2, float *red_n)
-{
-    const int t = threadIdx.x;
-    if (!MANY) {
-        red_mean[t] = mean[0];
-        red_M2[t] = M2[0];
-        red_n[t] = pieces * VEC;
-        return 1;
-    }
-    if (VEC % a.cpg == 0) {                            // whole groups of 1, 2 (or 4) channels: joined here
-        auto whole = [&](auto cpg) {
-            constexpr int W = decltype(cpg)::value;
-#pragma unroll
-            for (int g = 0; g < VEC / W; ++g) {
-                float d = 0.f, M = 0.f;
-#pragma unroll
-                for (int i = 1; i < W; ++i) d += mean[g * W + i] - mean[g * W];
-                const float centre = __fmaf_rn(d, 1.0f / W, mean[g * W]);
-#pragma unroll
-                for (int i = 0; i < W; ++i) { const float o = mean[g * W + i] - centre; M += __fmaf_rn(pieces * o, o, M2[g * W + i]); }
-                red_mean[t * (VEC / W) + g] = centre;
-                red_M2[t * (VEC / W) + g] = pieces > 0.f ? M : 0.f;
-            }
-            red_n[t] = pieces * W;
-            return VEC / W;
-        };
-        if (a.cpg == 2) return whole(std::integral_constant<int, 2>{});
-        if (VEC == 8 && a.cpg == 4) return whole(std::integral_constant<int, VEC == 8 ? 4 : 2>{});
-    }
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) { red_mean[t * VEC + i] = mean[i]; red_M2[t * VEC + i] = M2[i]; }
-    red_n[t] = pieces;
-    return VEC;
 }
 
 // A thread's pieces: its column and its position among those side by side; cpt > 1: its first column, at every position
@@ -462,6 +468,31 @@ template <int DT, int VEC, int NV, int DEPTH> struct PieceRing {
     }
 };
 
+// Of `bytes` that the blocks of the cluster will write: this block's barrier stands, and the others learn that it does (cluster_wait).
+__device__ __forceinline__ void announce(uint64_t *arrived, unsigned bytes)
+{
+    if (threadIdx.x == 0) {
+        ptx::mbar_init(arrived, 1);
+        ptx::fence_mbar_init();
+        ptx::mbar_expect_tx(arrived, bytes);
+    }
+    __syncthreads();
+    ptx::cluster_arrive();
+}
+__device__ __forceinline__ void wait_arrived(uint64_t *arrived)   // bounded: about two seconds
+{
+    bool here = ptx::mbar_try_wait(arrived, 0);
+    for (uint32_t i = 0; i < (1u << 21) && !here; ++i) here = ptx::mbar_try_wait_hint_s(ptx::smem_u32(arrived), 0, 1000u);   // (parked for a microsecond at most)
+    if (!here) atomicMax(&g_norm_status, 0x401u);
+}
+// k parts side by side in the lanes, this lane's with n of the `all` values
+__device__ __forceinline__ Moments join_cluster(float2 s, float n, float all, int k)
+{
+    const float centre = __fdiv_rn(part_sum(__fmul_rn(n, s.x), k), all), o = s.x - centre, no = n * o;
+    const float M = part_sum(__fmaf_rn(no, o, s.y), k), c = part_sum(no, k);
+    return Moments{all, centre + __fdividef(c, all), M};
+}
+
 // "held": block rank `blockIdx.x % cluster` of an image's channel block.  A thread's pieces lie in shared memory, [piece][thread]: in registers
 // the loops over them had to be unrolled, and fetching some thousands of instructions once each cost more than the memory.
 template <int DT, int VEC, bool MANY, int T>
@@ -477,15 +508,7 @@ __global__ void __launch_bounds__(T, 1024 / T) group_norm_held_kernel(const Norm
     // The blocks of a cluster write their groups' moments into one another's shared memory.  First each has to know that the others have begun
     // and their barriers stand: that is waited for below, while the data comes.  (Reading them from the others between two barriers
     // of the cluster was FIGURES slower.)
-    if (a.cluster_log) {
-        if (threadIdx.x == 0) {
-            ptx::mbar_init(&arrived, 1);
-            ptx::fence_mbar_init();
-            ptx::mbar_expect_tx(&arrived, (unsigned)(a.gpb << a.cluster_log) * 8u);
-        }
-        __syncthreads();
-        ptx::cluster_arrive();
-    }
+    if (a.cluster_log) announce(&arrived, (unsigned)(a.gpb << a.cluster_log) * 8u);
     // block (image and rank in the cluster, channel block)
     const int rank = (int)(blockIdx.x & ((1u << a.cluster_log) - 1u));
     const long long img = blockIdx.x >> a.cluster_log;
@@ -549,7 +572,8 @@ __global__ void __launch_bounds__(T, 1024 / T) group_norm_held_kernel(const Norm
         }
         squares_of<VEC, MANY>(q, M2);
     }
-    block_moments<VEC, MANY>(a, red_mean, red_M2, red_n, gstat, put_moments<VEC, MANY>(a, mean, M2, (float)cnt, red_mean, red_M2, red_n));
+    put_moments<VEC, MANY, T>(a, who.col, mean, M2, (float)cnt, red_mean, red_M2, red_n);
+    block_moments<VEC, MANY, T>(a, red_mean, red_M2, red_n, gstat);
     if (a.cluster_log) {
         // a thread per group and block of the cluster, those of a group side by side
         const int k = 1 << a.cluster_log, per = T >> a.cluster_log, r = threadIdx.x & (k - 1);
@@ -557,17 +581,13 @@ __global__ void __launch_bounds__(T, 1024 / T) group_norm_held_kernel(const Norm
         const uint32_t bar = ptx::mapa(ptx::smem_u32(&arrived), (uint32_t)r);
         for (int g = (int)(threadIdx.x >> a.cluster_log); g < a.gpb; g += per)
             ptx::st_async_64(ptx::mapa(ptx::smem_u32(&inbox[rank][g]), (uint32_t)r), gstat[g].mean, gstat[g].M2, bar);
-        bool here = ptx::mbar_try_wait(&arrived, 0);
-        for (uint32_t i = 0; i < (1u << 21) && !here; ++i) here = ptx::mbar_try_wait_hint_s(ptx::smem_u32(&arrived), 0, 1000u);   // (parked for a microsecond at most)
-        if (!here) atomicMax(&g_norm_status, 0x401u);
+        wait_arrived(&arrived);
         const long long other = a.P - r * a.span;              // positions of block r
         const float n = (float)((other < 0 ? 0 : other < a.span ? (int)other : (int)a.span) * a.cpg), all = (float)(a.P * a.cpg);
         for (int g0 = 0; g0 < a.gpb; g0 += per) {              // (all lanes stay: the sums need them)
             const int g = g0 + (int)(threadIdx.x >> a.cluster_log);
-            const float2 s = inbox[r][g < a.gpb ? g : 0];
-            const float centre = __fdiv_rn(part_sum(__fmul_rn(n, s.x), k), all), o = s.x - centre, no = n * o;
-            const float M = part_sum(__fmaf_rn(no, o, s.y), k), c = part_sum(no, k);
-            if (r == 0 && g < a.gpb) fin[g] = make_float2(centre + __fdividef(c, all), deviation_inverse(M, all, a.eps));
+            const Moments m = join_cluster(inbox[r][g < a.gpb ? g : 0], n, all, k);
+            if (r == 0 && g < a.gpb) fin[g] = make_float2(m.mean, deviation_inverse(m.M2, all, a.eps));
         }
     } else {
         for (int g = threadIdx.x; g < a.gpb; g += T) fin[g] = make_float2(gstat[g].mean, deviation_inverse(gstat[g].M2, gstat[g].n, a.eps));
@@ -633,6 +653,9 @@ __global__ void __launch_bounds__(kNormThreads, 2) group_norm_stats_kernel(const
     // block (image and piece, channel block)
     const long long img = blockIdx.x / (unsigned)a.cluster;
     const int part = (int)(blockIdx.x - (unsigned)img * (unsigned)a.cluster), block = (int)blockIdx.y, c0 = block * a.gpb * a.cpg;
+    __shared__ float2 inbox[kNormCluster][kMaxGroups];
+    __shared__ uint64_t arrived;
+    if (a.cluster_log) announce(&arrived, (unsigned)(a.gpb << a.cluster_log) * 8u);
     const long long p0 = part * a.span, left = a.P - p0;
     const int mine = (int)(left < 0 ? 0 : left < a.span ? left : a.span);
     const Place who(a);
@@ -718,9 +741,27 @@ __global__ void __launch_bounds__(kNormThreads, 2) group_norm_stats_kernel(const
         }
     }
     ptx::pdl_launch_dependents();
-    block_moments<VEC, MANY>(a, red_mean, red_M2, red_n, gstat, put_moments<VEC, MANY>(a, mean, M2, (float)cnt, red_mean, red_M2, red_n));
-    for (int g = threadIdx.x; g < a.gpb; g += blockDim.x)
-        a.stats[((size_t)img * a.groups + block * a.gpb + g) * a.cluster + part] = make_float2(gstat[g].mean, gstat[g].M2);
+    put_moments<VEC, MANY, kNormThreads>(a, who.col, mean, M2, (float)cnt, red_mean, red_M2, red_n);
+    block_moments<VEC, MANY, kNormThreads>(a, red_mean, red_M2, red_n, gstat);
+    float2 *const to = a.stats + ((size_t)img * a.groups + block * a.gpb) * a.joined + (part >> a.cluster_log);
+    if (a.cluster_log) {
+        // the first block of the cluster joins what the others write into its shared memory
+        const int k = 1 << a.cluster_log, rank = part & (k - 1), r = threadIdx.x & (k - 1), per = kNormThreads >> a.cluster_log;
+        ptx::cluster_wait();
+        const uint32_t bar = ptx::mapa(ptx::smem_u32(&arrived), 0);
+        for (int g = threadIdx.x; g < a.gpb; g += kNormThreads) ptx::st_async_64(ptx::mapa(ptx::smem_u32(&inbox[rank][g]), 0), gstat[g].mean, gstat[g].M2, bar);
+        if (rank) return;
+        wait_arrived(&arrived);
+        const long long other = a.P - (part + r) * a.span, here = a.P - part * a.span;
+        const float n = (float)((other < 0 ? 0 : other < a.span ? other : a.span) * a.cpg), all = (float)((here < a.span << a.cluster_log ? here : a.span << a.cluster_log) * a.cpg);
+        for (int g0 = 0; g0 < a.gpb; g0 += per) {              // (all lanes stay: the sums need them)
+            const int g = g0 + (int)(threadIdx.x >> a.cluster_log);
+            const Moments m = join_cluster(inbox[r][g < a.gpb ? g : 0], n, all, k);
+            if (r == 0 && g < a.gpb) to[(size_t)g * a.joined] = make_float2(m.mean, m.M2);
+        }
+    } else {
+        for (int g = threadIdx.x; g < a.gpb; g += kNormThreads) to[(size_t)g * a.joined] = make_float2(gstat[g].mean, gstat[g].M2);
+    }
 }
 
 // "twice", the second: the pieces' moments joined, and the values.  Blocks in reverse order: what was read last is in the L2 cache.
@@ -732,24 +773,25 @@ __global__ void __launch_bounds__(kNormThreads, 3) group_norm_apply_kernel(const
     extern __shared__ __align__(16) uint8_t hold_bytes[];
     __shared__ float2 fin[kMaxGroups];
     const unsigned id = gridDim.x - 1 - blockIdx.x;
-    const long long img = id / (unsigned)a.cluster;
-    const int part = (int)(id - (unsigned)img * (unsigned)a.cluster), block = (int)(gridDim.y - 1 - blockIdx.y), c0 = block * a.gpb * a.cpg;
-    const long long p0 = part * a.span, left = a.P - p0;
-    const int mine = (int)(left < 0 ? 0 : left < a.span ? left : a.span);
+    const long long img = id / (unsigned)a.cuts;
+    const int part = (int)(id - (unsigned)img * (unsigned)a.cuts), block = (int)(gridDim.y - 1 - blockIdx.y), c0 = block * a.gpb * a.cpg;
+    const long long p0 = part * a.cut_span, left = a.P - p0;
+    const int mine = (int)(left < 0 ? 0 : left < a.cut_span ? left : a.cut_span);
     const Place who(a);
     const int lane = threadIdx.x & 31;
     ptx::pdl_wait();
     for (int g = threadIdx.x >> 5; g < a.gpb; g += (int)blockDim.x >> 5) {
-        const float2 *from = a.stats + ((size_t)img * a.groups + block * a.gpb + g) * a.cluster;
+        const float2 *from = a.stats + ((size_t)img * a.groups + block * a.gpb + g) * a.joined;
         float d = 0.f, M2 = 0.f, c = 0.f;
-        const float all = (float)(a.P * a.cpg), each = (float)(a.span * a.cpg);
+        const long long span = a.span << a.cluster_log;        // positions of one of them
+        const float all = (float)(a.P * a.cpg), each = (float)(span * a.cpg);
         auto weight = [&](int i) {                             // values of piece i
-            const long long rest = a.P - i * a.span;
-            return rest >= a.span ? each : rest > 0 ? (float)(rest * a.cpg) : 0.f;
+            const long long rest = a.P - i * span;
+            return rest >= span ? each : rest > 0 ? (float)(rest * a.cpg) : 0.f;
         };
-        for (int i = lane; i < a.cluster; i += 32) d = __fmaf_rn(weight(i), from[i].x, d);
+        for (int i = lane; i < a.joined; i += 32) d = __fmaf_rn(weight(i), from[i].x, d);
         const float centre = __fdiv_rn(warp_sum(d), all);
-        for (int i = lane; i < a.cluster; i += 32) {
+        for (int i = lane; i < a.joined; i += 32) {
             const float2 s = from[i];
             const float w = weight(i), q = s.x - centre, wq = w * q;
             c += wq;
@@ -808,22 +850,36 @@ __global__ void __launch_bounds__(kNormThreads, 3) group_norm_apply_kernel(const
 // "rows": one position per image.  A warp takes a group at a time (its cpg values are contiguous) and has the next kRowDepth - 1 on the way, in shared
 // memory of its own; gamma and beta stay in registers where it meets the same channels again (one group, or a stride of whole rows).  NV is the
 // number of a lane's pieces exactly, so that only the last may be missing: with a test on every piece a third of the instructions were branches.
+// Long groups are taken by WARPS warps together, which exchange their sums.
 constexpr int kRowDepth = 4;
-template <int DT, int VEC, int NV>
+template <int DT, int VEC, int NV, int WARPS>
 __global__ void __launch_bounds__(kNormThreads, NV == 1 ? 3 : 2) group_norm_rows_kernel(const NormArgs a)
 {
-    constexpr int kPairs = VEC == 1 ? 1 : VEC / 2, kSlot = NV * 32 * (VEC == 1 ? 4 : 16);
-    constexpr bool kKeep = NV * VEC <= 24;
+    constexpr int kPairs = VEC == 1 ? 1 : VEC / 2, kLanes = 32 * WARPS, kSlot = NV * kLanes * (VEC == 1 ? 4 : 16), kTeams = kNormThreads / kLanes;
+    constexpr bool kKeep = NV * VEC <= 32;
     typedef Piece<DT, VEC> P;
     extern __shared__ __align__(16) uint8_t hold_bytes[];
-    const int lane = threadIdx.x & 31;
-    const int total = (int)(a.Nb * a.groups), step = (int)(gridDim.x * (blockDim.x >> 5));   // (the host takes no more than 2^31 of them)
-    int seg = (int)(blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5));
-    const bool last = lane + 32 * (NV - 1) < a.nch;
+    __shared__ float part[2][kTeams][WARPS];
+    const int lane = (int)threadIdx.x % kLanes, team = (int)threadIdx.x / kLanes, teams = (int)blockDim.x / kLanes;
+    const int total = (int)(a.Nb * a.groups), step = (int)gridDim.x * teams;   // (the host takes no more than 2^30 of them)
+    int seg = (int)blockIdx.x * teams + team;
+    const bool last = lane + kLanes * (NV - 1) < a.nch;
+    // over the team's lanes; `which`: the two sums of a group, whose places are free again by the next one's
+    auto sum = [&](float v, int which) {
+        v = warp_sum(v);
+        if constexpr (WARPS > 1) {
+            if ((threadIdx.x & 31) == 0) part[which][team][lane >> 5] = v;
+            asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "n"(kLanes) : "memory");
+            v = part[which][team][0];
+#pragma unroll
+            for (int w = 1; w < WARPS; ++w) v += part[which][team][w];
+        }
+        return v;
+    };
     ptx::pdl_wait();
     if (seg >= total) return;
-    // [group of the warp][piece][lane]
-    uint8_t *const hold = hold_bytes + (threadIdx.x >> 5) * (kRowDepth * kSlot) + lane * (VEC == 1 ? 4 : 16);
+    // [team][group][piece][lane]
+    uint8_t *const hold = hold_bytes + team * (kRowDepth * kSlot) + lane * (VEC == 1 ? 4 : 16);
     const char *from = static_cast<const char *>(a.X) + ((size_t)seg * a.cpg + lane * VEC) * P::kBytes;
     const size_t stride = (size_t)step * a.cpg * P::kBytes;
     auto request = [&](bool there, int slot) {             // (an empty batch of copies where there is no such group)
@@ -831,13 +887,13 @@ __global__ void __launch_bounds__(kNormThreads, NV == 1 ? 3 : 2) group_norm_rows
 #pragma unroll
             for (int j = 0; j < NV; ++j)
                 if (j < NV - 1 || last) {
-                    uint8_t *const to = hold + slot + j * 32 * (VEC == 1 ? 4 : 16);
+                    uint8_t *const to = hold + slot + j * kLanes * (VEC == 1 ? 4 : 16);
                     if constexpr (VEC == 1) {
                         P v;
-                        v.load(from + j * 32 * VEC * P::kBytes);
+                        v.load(from + j * kLanes * VEC * P::kBytes);
                         *reinterpret_cast<float *>(to) = v.raw;
                     } else {
-                        ptx::cp_async_16(ptx::smem_u32(to), from + j * 32 * VEC * P::kBytes);
+                        ptx::cp_async_16(ptx::smem_u32(to), from + j * kLanes * VEC * P::kBytes);
                     }
                 }
         }
@@ -851,7 +907,7 @@ __global__ void __launch_bounds__(kNormThreads, NV == 1 ? 3 : 2) group_norm_rows
     int shift[NV], ent[NV], held = -1;
 #pragma unroll
     for (int j = 0; j < NV; ++j) shift[j] = ent[j] = 0;
-    const int ob = out_bytes(a.out), next_piece = 32 * VEC * ob;
+    const int ob = out_bytes(a.out), next_piece = kLanes * VEC * ob;
     char *to = static_cast<char *>(a.out.Y) + ((size_t)seg * a.cpg + lane * VEC) * ob;
     const size_t far = (size_t)step * a.cpg * ob;
     const float count = (float)a.cpg, inverse = __frcp_rn(count);
@@ -864,7 +920,7 @@ __global__ void __launch_bounds__(kNormThreads, NV == 1 ? 3 : 2) group_norm_rows
         for (int j = 0; j < NV; ++j)
             if (j < NV - 1 || last) {
                 P v;
-                v.raw = *reinterpret_cast<const typename P::Raw *>(hold + slot + j * 32 * (VEC == 1 ? 4 : 16));
+                v.raw = *reinterpret_cast<const typename P::Raw *>(hold + slot + j * kLanes * (VEC == 1 ? 4 : 16));
                 v.widen(x[j]);
             } else {
 #pragma unroll
@@ -877,7 +933,7 @@ __global__ void __launch_bounds__(kNormThreads, NV == 1 ? 3 : 2) group_norm_rows
             for (int j = 1; j < NV; ++j) s[i] = add2(s[i], x[j][i]);
         }
         slot = slot == (kRowDepth - 1) * kSlot ? 0 : slot + kSlot;
-        const float mean = divide(warp_sum(fold<kPairs>(s)), count, inverse);
+        const float mean = divide(sum(fold<kPairs>(s), 0), count, inverse);
         const pair_t minus = pair(-mean, VEC == 1 ? 0.f : -mean), minus_last = last ? minus : pair(0.f, 0.f);
 #pragma unroll
         for (int i = 0; i < kPairs; ++i) {
@@ -893,16 +949,16 @@ __global__ void __launch_bounds__(kNormThreads, NV == 1 ? 3 : 2) group_norm_rows
 #pragma unroll
             for (int j = 0; j < NV; ++j)
                 if (j < NV - 1 || last) {
-                    const int c = g * a.cpg + (lane + 32 * j) * VEC;
+                    const int c = g * a.cpg + (lane + kLanes * j) * VEC;
                     if (kKeep) load_affine<VEC>(a, c, gamma[kKeep ? j : 0], beta[kKeep ? j : 0]);
                     shift[j] = slab_shift(a.out, c, &ent[j]);
                 }
         }
-        const float rstd = deviation_inverse(warp_sum(fold<kPairs>(s)), count, a.eps);
+        const float rstd = deviation_inverse(sum(fold<kPairs>(s), 1), count, a.eps);
         const pair_t r = pair(rstd, rstd);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            if (!kKeep && (j < NV - 1 || last)) load_affine<VEC>(a, g * a.cpg + (lane + 32 * j) * VEC, gamma[0], beta[0]);
+            if (!kKeep && (j < NV - 1 || last)) load_affine<VEC>(a, g * a.cpg + (lane + kLanes * j) * VEC, gamma[0], beta[0]);
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) x[j][i] = fma2(x[j][i], mul2(gamma[kKeep ? j : 0][i], r), beta[kKeep ? j : 0][i]);
         }
@@ -925,6 +981,15 @@ template <class K> static int allow_smem(K kernel, bool (&done)[64], int bytes)
     if (dev < 64) done[dev] = true;
     return FLEXIQ_OK;
 }
+static void set_attributes(cudaLaunchAttribute *attr, unsigned cluster)
+{
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+}
 template <int DT, int VEC, bool MANY, int T> static int launch_held_threads(const NormArgs &a, const NormPlan &p, cudaStream_t st)
 {
     static bool done[64] = {};
@@ -935,12 +1000,7 @@ template <int DT, int VEC, bool MANY, int T> static int launch_held_threads(cons
     cfg.dynamicSmemBytes = (size_t)p.nv * T * (VEC == 1 ? 4 : 16);
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = 1u << a.cluster_log;
-    attr[1].val.clusterDim.y = 1;
-    attr[1].val.clusterDim.z = 1;
+    set_attributes(attr, 1u << a.cluster_log);
     cfg.attrs = attr;
     cfg.numAttrs = a.cluster_log ? 2 : 1;
     FLEXIQ_CUDA_TRY(cudaLaunchKernelEx(&cfg, group_norm_held_kernel<DT, VEC, MANY, T>, a));
@@ -957,40 +1017,59 @@ template <int DT, int VEC, bool MANY> static int launch_held(const NormArgs &a, 
 }
 template <int DT, int VEC, bool MANY> static int launch_twice(const NormArgs &a, const NormPlan &p, cudaStream_t st)
 {
-    const dim3 grid((unsigned)(a.Nb * a.cluster), (unsigned)(a.groups / a.gpb), 1);
+    const unsigned blocks = (unsigned)(a.groups / a.gpb);
     constexpr int kStats = kNormThreads * kStatsPieces * kStatsDepth * (VEC == 1 ? 4 : 16), kApply = kNormThreads * kApplyPieces * kApplyDepth * (VEC == 1 ? 4 : 16);
     static bool done[2][64] = {};
     if (int rc = allow_smem(group_norm_stats_kernel<DT, VEC, MANY>, done[0], kStats)) return rc;
     if (int rc = allow_smem(group_norm_apply_kernel<DT, VEC, MANY>, done[1], kApply)) return rc;
-    FLEXIQ_CUDA_TRY(launch_pdl(group_norm_stats_kernel<DT, VEC, MANY>, grid, (unsigned)p.threads, kStats, st, a));
-    FLEXIQ_CUDA_TRY(launch_pdl(group_norm_apply_kernel<DT, VEC, MANY>, grid, (unsigned)p.threads, kApply, st, a));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(a.Nb * a.cluster), blocks, 1);
+    cfg.blockDim = dim3((unsigned)p.threads, 1, 1);
+    cfg.dynamicSmemBytes = kStats;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    set_attributes(attr, 1u << a.cluster_log);
+    cfg.attrs = attr;
+    cfg.numAttrs = a.cluster_log ? 2 : 1;
+    FLEXIQ_CUDA_TRY(cudaLaunchKernelEx(&cfg, group_norm_stats_kernel<DT, VEC, MANY>, a));
+    FLEXIQ_CUDA_TRY(launch_pdl(group_norm_apply_kernel<DT, VEC, MANY>, dim3((unsigned)(a.Nb * a.cuts), blocks, 1), (unsigned)p.threads, kApply, st, a));
     return FLEXIQ_OK;
 }
-template <int DT, int VEC, int NV> static int launch_rows_nv(const NormArgs &a, int sms, cudaStream_t st)
+template <int DT, int VEC, int NV, int WARPS> static int launch_rows_nv(const NormArgs &a, int sms, cudaStream_t st)
 {
-    // few rows: as many blocks as there are; many: as many blocks of eight warps as an SM holds, each warp walking over rows
+    // few rows: as many blocks as there are; many: as many blocks of eight warps as an SM holds, each team of warps walking over rows
     const long long total = a.Nb * a.groups;
-    const unsigned threads = total < 8ll * sms ? 64 : kNormThreads;
-    long long blocks = ceil_div(total, threads / 32);
+    const unsigned threads = total < 8ll * sms ? (WARPS > 2 ? 32 * WARPS : 64) : kNormThreads;
+    long long blocks = ceil_div(total, threads / (32 * WARPS));
     const long long most = (NV == 1 ? 3ll : 2ll) * sms;
     if (blocks > most && threads == kNormThreads) blocks = most;
     constexpr int kRow = kRowDepth * NV * (VEC == 1 ? 4 : 16);   // a thread's slots
     static bool done[64] = {};
-    if (int rc = allow_smem(group_norm_rows_kernel<DT, VEC, NV>, done, kNormThreads * kRow)) return rc;
-    FLEXIQ_CUDA_TRY(launch_pdl(group_norm_rows_kernel<DT, VEC, NV>, (unsigned)blocks, threads, (size_t)threads * kRow, st, a));
+    if (int rc = allow_smem(group_norm_rows_kernel<DT, VEC, NV, WARPS>, done, kNormThreads * kRow)) return rc;
+    FLEXIQ_CUDA_TRY(launch_pdl(group_norm_rows_kernel<DT, VEC, NV, WARPS>, (unsigned)blocks, threads, (size_t)threads * kRow, st, a));
     return FLEXIQ_OK;
 }
 template <int DT, int VEC> static int launch_norm_rows(const NormArgs &a, const NormPlan &p, int sms, cudaStream_t st)
 {
+    if constexpr (VEC > 1) {
+        if (p.warps > 1) switch (p.nv) {
+            case 3: return launch_rows_nv<DT, VEC, 3, kRowWarps>(a, sms, st);
+            case 4: return launch_rows_nv<DT, VEC, 4, kRowWarps>(a, sms, st);
+            case 5: return launch_rows_nv<DT, VEC, 5, kRowWarps>(a, sms, st);
+            case 6: return launch_rows_nv<DT, VEC, 6, kRowWarps>(a, sms, st);
+            case 7: return launch_rows_nv<DT, VEC, 7, kRowWarps>(a, sms, st);
+            default: return launch_rows_nv<DT, VEC, 8, kRowWarps>(a, sms, st);
+        }
+    }
     switch (p.nv) {
-        case 1: return launch_rows_nv<DT, VEC, 1>(a, sms, st);
-        case 2: return launch_rows_nv<DT, VEC, 2>(a, sms, st);
-        case 3: return launch_rows_nv<DT, VEC, 3>(a, sms, st);
-        case 4: return launch_rows_nv<DT, VEC, 4>(a, sms, st);
-        case 5: return launch_rows_nv<DT, VEC, 5>(a, sms, st);
-        case 6: return launch_rows_nv<DT, VEC, 6>(a, sms, st);
-        case 7: return launch_rows_nv<DT, VEC, 7>(a, sms, st);
-        default: return launch_rows_nv<DT, VEC, 8>(a, sms, st);
+        case 1: return launch_rows_nv<DT, VEC, 1, 1>(a, sms, st);
+        case 2: return launch_rows_nv<DT, VEC, 2, 1>(a, sms, st);
+        case 3: return launch_rows_nv<DT, VEC, 3, 1>(a, sms, st);
+        case 4: return launch_rows_nv<DT, VEC, 4, 1>(a, sms, st);
+        case 5: return launch_rows_nv<DT, VEC, 5, 1>(a, sms, st);
+        case 6: return launch_rows_nv<DT, VEC, 6, 1>(a, sms, st);
+        case 7: return launch_rows_nv<DT, VEC, 7, 1>(a, sms, st);
+        default: return launch_rows_nv<DT, VEC, 8, 1>(a, sms, st);
     }
 }
 template <int DT> static int launch_norm(const NormArgs &a, const NormPlan &p, int sms, cudaStream_t st)
@@ -1041,24 +1120,22 @@ static int plan_sms()
     const int n = device_sm_count(dev);
     return n > 0 ? n : 148;
 }
-static long long scratch_bytes(const NormPlan &p, long long Nb, int groups) { return p.kind == kNormTwice ? Nb * groups * p.cluster * (long long)sizeof(float2) : 0; }
+static long long scratch_bytes(const NormPlan &p, long long Nb, int groups) { return p.kind == kNormTwice ? Nb * groups * (p.cluster >> p.cluster_log) * (long long)sizeof(float2) : 0; }
 
 static int run_norm(NormArgs &a, int x_dtype, void *scratch, cudaStream_t st)
 {
     const int sms = plan_sms();
     const NormPlan p = plan_norm(x_dtype, a.Nb, a.P, a.C, a.groups, sms);
-    if ((p.kind == kNormRows ? a.Nb * a.groups : a.Nb * (long long)p.cluster) > 0x40000000ll || (p.kind != kNormRows && a.groups / p.gpb > 65535))
+    if ((p.kind == kNormRows ? a.Nb * a.groups : a.Nb * (long long)(p.cluster > p.cuts ? p.cluster : p.cuts)) > 0x40000000ll || (p.kind != kNormRows && a.groups / p.gpb > 65535))
         return set_error(FLEXIQ_ERR_UNSUPPORTED, "too many images and groups for one launch");
     if (p.kind == kNormTwice && (!scratch || (reinterpret_cast<uintptr_t>(scratch) & 15)))
         return set_error(FLEXIQ_ERR_INVALID_ARG, "scratch_dev is NULL or not 16-byte aligned: this shape needs %lld bytes", scratch_bytes(p, a.Nb, a.groups));
     a.cpg = a.C / a.groups;
-    a.gpb = p.gpb; a.nch = p.nch; a.cpt = p.cpt; a.lanes = p.lanes; a.cluster = p.cluster; a.span = p.span;
+    a.gpb = p.gpb; a.nch = p.nch; a.cpt = p.cpt; a.lanes = p.lanes; a.cluster = p.cluster; a.span = p.span; a.cuts = p.cuts; a.cut_span = p.cut_span;
     a.stats = static_cast<float2 *>(scratch);
-    for (a.cluster_log = 0; (1 << a.cluster_log) < p.cluster; ++a.cluster_log) {}
+    a.cluster_log = p.cluster_log; a.joined = p.cluster >> p.cluster_log;
     auto inverse = [](int d) { return d > 1 ? (unsigned)((0x100000000ull + d - 1) / d) : 0u; };   // (exact for numerators below 2^16 and such d)
-    const int sub = p.many && p.vec % a.cpg == 0 && a.cpg > 1 ? p.vec / a.cpg : p.many ? p.vec : 1;
-    const int each = p.cpt > 1 ? kNormThreads : p.many ? (sub < p.vec ? 1 : a.cpg) : a.cpg / p.vec;
-    a.by_nch = inverse(p.nch); a.by_lanes = inverse(p.lanes); a.by_cpg = inverse(a.cpg); a.by_each = inverse(each);
+    a.by_nch = inverse(p.nch); a.by_lanes = inverse(p.lanes); a.by_cpg = inverse(a.cpg);
     switch (x_dtype) {
         case FLEXIQ_DTYPE_F32: return launch_norm<FLEXIQ_DTYPE_F32>(a, p, sms, st);
         case FLEXIQ_DTYPE_F16: return launch_norm<FLEXIQ_DTYPE_F16>(a, p, sms, st);

@@ -5,13 +5,14 @@
 namespace flexiq {
 
 constexpr int kNormThreads = 256;
+constexpr int kRowWarps = 4;           // warps that take a long row together
 constexpr int kNormHold = 65536;        // bytes a block holds ("held")
 constexpr int kNormCluster = 8;        // blocks of a cluster at most ("held")
-constexpr int kNormSplits = 256;       // pieces of an image's channel block at most ("twice")
+constexpr int kNormSplits = 512;       // pieces of an image's channel block at most ("twice")
 constexpr int kMaxGroups = 128;        // groups of a channel block at most
 
 enum NormKind { kNormRows, kNormHeld, kNormTwice };
-struct NormPlan { NormKind kind; int vec, nv, threads, gpb, nch, cpt, lanes, cluster; long long span; bool many; };
+struct NormPlan { NormKind kind; int vec, nv, warps, threads, gpb, nch, cpt, lanes, cluster, cluster_log, cuts; long long span, cut_span; bool many; };
 
 inline int gcd(int a, int b) { while (b) { const int t = a % b; a = b; b = t; } return a; }
 inline long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
@@ -24,9 +25,11 @@ inline NormPlan plan_norm(int x_dtype, long long Nb, long long P, int C, int gro
     NormPlan p{};
     p.cpt = 1;
     if (P == 1) {
-        const int vec = cpg % full == 0 ? full : 1, nv = (int)ceil_div(cpg / vec, 32);
-        if (nv <= 8) {
-            p.kind = kNormRows; p.vec = vec; p.nv = nv; p.nch = cpg / vec;
+        const int vec = cpg % full == 0 ? full : 1, pieces = cpg / vec;
+        p.warps = pieces <= 256 ? 1 : kRowWarps;
+        p.nv = (int)ceil_div(pieces, 32 * p.warps);
+        if (p.nv <= 8 && (vec > 1 || p.warps == 1)) {
+            p.kind = kNormRows; p.vec = vec; p.nch = pieces;
             return p;
         }
     }
@@ -61,6 +64,7 @@ inline NormPlan plan_norm(int x_dtype, long long Nb, long long P, int C, int gro
         // more blocks where the machine has room for them and a thread more than one piece
         while (k < kNormCluster && blocks * k * 2 <= 2 * sms && ceil_div(P, k) > (p.cpt > 1 ? 1 : kNormThreads / p.nch)) k *= 2;
         p.cluster = k;
+        for (p.cluster_log = 0; (1 << p.cluster_log) < k; ++p.cluster_log) {}
         p.span = ceil_div(P, k);
         if (p.cpt == 1) {
             // threads for about four pieces each: the passes over them are a chain of latencies.  Where there are blocks for every SM a thread's fixed
@@ -82,17 +86,24 @@ inline NormPlan plan_norm(int x_dtype, long long Nb, long long P, int C, int gro
     p.kind = kNormTwice;
     p.threads = kNormThreads;
     p.lanes = p.cpt > 1 ? 1 : kNormThreads / p.nch;
-    // pieces: as many as make whole waves of two blocks an SM (nine tenths of one at least, where up to four waves allow that), and a few steps each
-    const long long blocks = Nb * (units / m), steps = p.cpt > 1 ? P : ceil_div(P, (long long)p.lanes * 8), wave = 2ll * sms;
-    long long k = 1;
-    for (long long w = 1; w <= 4; ++w) {
-        k = w * wave / blocks;
-        if (k * blocks * 10 >= w * wave * 9) break;
-    }
-    if (k > steps) k = steps;
-    if (k > kNormSplits) k = kNormSplits;
-    p.cluster = (int)(k < 1 ? 1 : k);
+    // Pieces: as many as make whole waves of the blocks that fit an SM (nine tenths of one at least, where up to four waves allow that), and a few
+    // steps each.  Two blocks fit with the statistics' registers, three with those of the second kernel, which cuts the image anew.
+    const long long blocks = Nb * (units / m), steps = p.cpt > 1 ? P : ceil_div(P, (long long)p.lanes * 8);
+    auto pieces = [&](long long wave) {
+        long long k = 1;
+        for (long long w = 1; w <= 4; ++w) {
+            k = w * wave / blocks;
+            if (k * blocks * 10 >= w * wave * 9) break;
+        }
+        k = k < steps ? k : steps;
+        return (int)(k < 1 ? 1 : k < kNormSplits ? k : kNormSplits);
+    };
+    p.cluster = pieces(2ll * sms);
+    p.cluster_log = p.cluster > 128 ? 2 : 0;   // the statistics of four pieces are joined where they are made (clusters of eight found no room: FIGURES)
+    p.cluster &= ~((1 << p.cluster_log) - 1);
     p.span = ceil_div(P, p.cluster);
+    p.cuts = pieces(3ll * sms);
+    p.cut_span = ceil_div(P, p.cuts);
     return p;
 }
 

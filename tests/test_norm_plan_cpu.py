@@ -19,7 +19,8 @@ static int check(int dt, long long Nb, long long P, int C, int groups)
     auto bad = [&](const char *w) { return fail(w, dt, Nb, P, C, groups); };
     if (p.vec != 1 && (p.vec != full || C % full)) return bad("width");
     if (p.kind == kNormRows) {
-        if (P != 1 || p.nch * p.vec != cpg || p.nv * 32 < p.nch || p.nv > 8 || p.nv < 1) return bad("rows");
+        if (P != 1 || p.nch * p.vec != cpg || p.nv * 32 * p.warps < p.nch || (p.nv - 1) * 32 * p.warps >= p.nch || p.nv > 8 || p.nv < 1) return bad("rows");
+        if (p.warps != 1 && (p.warps != kRowWarps || p.vec == 1 || p.nv < 3)) return bad("warps of a row");
         return 0;
     }
     if (p.gpb < 1 || groups % p.gpb || p.gpb > kMaxGroups || p.nch * p.vec != p.gpb * cpg) return bad("channel block");
@@ -29,6 +30,7 @@ static int check(int dt, long long Nb, long long P, int C, int groups)
     if (p.cpt > 1 && (p.gpb != 1 || p.many || p.threads != kNormThreads || p.lanes != 1 || p.cpt * p.threads < p.nch)) return bad("wide positions");
     if (p.cpt == 1 && (p.lanes < 1 || p.lanes * p.nch > p.threads)) return bad("lanes");
     if (p.cluster < 1 || p.cluster > (p.kind == kNormHeld ? kNormCluster : kNormSplits) || p.span * p.cluster < P || p.span < 1) return bad("pieces of an image");
+    if (p.kind == kNormTwice && (p.cuts < 1 || p.cuts > kNormSplits || p.cut_span * p.cuts < P || p.cut_span < 1)) return bad("the second kernel's pieces");
     if (p.kind == kNormHeld) {
         if ((p.cluster & (p.cluster - 1)) || p.nv < 1 || p.nv * p.threads * 16 > kNormHold || (p.threads != 64 && p.threads != 128 && p.threads != 256 && p.threads != 512)) return bad("what a block holds");
         std::vector<unsigned char> seen((size_t)p.span * p.nch, 0);
@@ -51,8 +53,24 @@ static int check(int dt, long long Nb, long long P, int C, int groups)
             if ((inv ? (int)(((unsigned long long)n * inv) >> 32) : n) != n / d) return bad("quotients by multiplication");
     }
     ++r0;
-    const int S = p.many ? p.vec : 1, pitch = p.cpt > 1 ? p.threads : p.nch * S, each = p.cpt > 1 ? p.threads : (p.many ? cpg : cpg / p.vec);
-    if ((p.lanes - 1) * pitch + p.gpb * each > p.threads * S) return bad("entries");
+    if (p.cluster_log < 0 || p.cluster % (1 << p.cluster_log) || (p.kind == kNormHeld && p.cluster != 1 << p.cluster_log)) return bad("clusters");
+    // entries: every group's, from the columns that hold a part of it, are those its threads have put
+    if (p.many) {
+        std::vector<int> has((size_t)p.gpb, 0);
+        for (int col = 0; col < p.nch; ++col) {
+            int left = cpg - (col * p.vec - col * p.vec / cpg * cpg), w = 0;
+            for (int i = 0; i < p.vec; ++i)
+                if (--left == 0 || i == p.vec - 1) {
+                    if (w >= p.vec) return bad("entries of a thread");
+                    const int g = col * p.vec / cpg + w++;
+                    if (g >= p.gpb || col < g * cpg / p.vec || col > ((g + 1) * cpg - 1) / p.vec) return bad("an entry of no group");
+                    ++has[g];
+                    left = cpg;
+                }
+        }
+        for (int g = 0; g < p.gpb; ++g)
+            if (has[g] != ((g + 1) * cpg - 1) / p.vec - g * cpg / p.vec + 1) return bad("columns of a group");
+    }
     return 0;
 }
 int main()
