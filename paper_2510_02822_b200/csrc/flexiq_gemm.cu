@@ -579,8 +579,6 @@ __device__ __forceinline__ void epilogue_role(const GemmParams &p, const Epilogu
                 // 16 columns at a time
                 const int units = cols >> 4;
                 ResidualUnit res = {};
-                uint32_t chunk[8] = {};                            // scattered: the even unit's chunk, and the odd one's
-                int held_pos = 0;
 #pragma unroll 1
                 for (int u = 0; u < units; ++u) {
                     const int n = nw + 16 * u;
@@ -638,23 +636,24 @@ __device__ __forceinline__ void epilogue_role(const GemmParams &p, const Epilogu
                     float v[16];
                     finish16_act<RES>(p, r, x.fac + 16 * u, x.fac + 64 + 16 * u, res, v);
                     if (kScatterOut) {
+                        // a chunk is a box of 16 columns wherever it goes; two of them are under way (768 -> 3072 at 12,608 rows into slab order of 16-channel
+                        // groups: 29.7 us, by 16-byte stores from the lanes 34.6; with GELU 40.1 and 42.8)
                         const int ent_u = u == 0 ? ents[0] : u == 1 ? ents[1] : u == 2 ? ents[2] : ents[3];
-                        quantize16_next(p, ent_u, v, chunk + 4);
-                        const int pos = ent_u & 0xffffff;
-                        if (row < p.M) {
-                            // chunks that lie side by side in the slab too go out as one whole sector
-                            const bool held = u & 1, hold = !held && n + 16 < p.N;
-                            uint8_t *srow = static_cast<uint8_t *>(p.Y) + row * p.N;
-                            if (held && pos == held_pos + 1 && (held_pos & 1) == 0 && ((reinterpret_cast<uintptr_t>(p.Y) | (uintptr_t)p.N) & 31) == 0)
-                                st_global_256(srow + held_pos * 16, chunk);
-                            else {
-                                if (held) st_global_128(srow + held_pos * 16, chunk[0], chunk[1], chunk[2], chunk[3]);
-                                if (!hold) st_global_128(srow + pos * 16, chunk[4], chunk[5], chunk[6], chunk[7]);
-                            }
+                        uint32_t w[4];
+                        quantize16_next(p, ent_u, v, w);
+                        const uint32_t half = x.store_stage + (uint32_t)(u & 1) * 512u;
+                        if (lane == 0) ptx::bulk_wait_read<1>();         // the store before the previous one has read its buffer
+                        __syncwarp();
+                        ptx::st_shared_128(half + (uint32_t)lane * 16u, w[0], w[1], w[2], w[3]);
+                        ptx::fence_proxy_async_smem();
+                        __syncwarp();
+                        if (lane == 0) {
+                            const int col = (ent_u & 0xffffff) * 16;
+                            if (KIND == 3) ptx::tma_store_4d(x.map_y16, half, col, st_x, st_n, st_y);
+                            else if (kGrid) ptx::tma_store_4d(x.map_y16, half, col, st_x, st_y, st_n);
+                            else ptx::tma_store_2d(x.map_y16, half, col, (int)row0);
+                            ptx::bulk_commit_group();
                         }
-                        held_pos = pos;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) chunk[i] = chunk[4 + i];
                         continue;
                     }
                     const uint32_t dst = x.store_stage + (uint32_t)lane * 32u, sw16 = ((uint32_t)lane >> 2 & 1u) << 4;
@@ -851,7 +850,7 @@ __device__ __forceinline__ void epilogue_role(const GemmParams &p, const Epilogu
         }
         if (!kPatch && (buf ^= 1) == 0) buf_phase ^= 1;
     }
-    if (kStaged && lane == 0) ptx::bulk_wait_all();  // the staged stores are performed
+    if ((kStaged || ACT) && lane == 0) ptx::bulk_wait_all();  // the staged stores are performed
     if (quad == 2 && part == 0 && lane == 0) { PROF_STORE(8, prof_wait); PROF_STORE(9, clock64() - prof_start); PROF_STORE(10, prof_ld); PROF_STORE(11, prof_math); }
 }
 
@@ -2172,11 +2171,11 @@ static int run_mixed(Layer *L, const uint8_t *X4, const int8_t *X8, const uint8_
     const bool half_out = out_mode == FLEXIQ_OUT_DEQUANT_F16 || out_mode == FLEXIQ_OUT_DEQUANT_BF16;
     const bool word_out = out_mode == FLEXIQ_OUT_DEQUANT_F32 || out_mode == FLEXIQ_OUT_ACC_I32;
     const int y_elem = half_out ? 2 : (word_out ? 4 : 1);
-    const bool staged = !next || out_order == FLEXIQ_ORDER_NEXT_SLAB;
+    const bool staged = !next || out_order == FLEXIQ_ORDER_NEXT_SLAB, mapped = staged || ops;   // (an activation's scattered chunks are boxes too)
     const void *slab = packed_path ? static_cast<const void *>(X8) : static_cast<const void *>(X4);
     Layer::CallMaps &cm = L->call_maps;
     const bool cached = !packed && cm.slab == slab && cm.M == M && cm.Nb == Nb && cm.H == H && cm.W == W && cm.bk == p.BK &&
-                        cm.im2col == (int)p.im2col + 2 * (int)patch + 4 * (int)stream && (!staged || (cm.staged && cm.Y == Y && cm.y_elem == y_elem));
+                        cm.im2col == (int)p.im2col + 2 * (int)patch + 4 * (int)stream && (!mapped || (cm.staged && cm.Y == Y && cm.y_elem == y_elem));
     if (cached) {
         a_lo = a_hi = cm.a;
     } else if (!packed) {
@@ -2209,34 +2208,34 @@ static int run_mixed(Layer *L, const uint8_t *X4, const int8_t *X8, const uint8_
     }
     // int8 output leaves through staged tiled bulk stores
     CUtensorMap y_map = a_hi, y_map16 = a_hi;
-    if (staged && cached) {
+    if (mapped && cached) {
         y_map = cm.y;
         y_map16 = cm.y16;
-    } else if (staged && patch) {
+    } else if (mapped && patch) {
         // a warp's 32 accumulator rows are bx consecutive pixels of by consecutive output rows
         const uint32_t bx = (1u << p.pw_log2) < 32u ? (1u << p.pw_log2) : 32u, by = 32u / bx;
         const uint64_t rb = (uint64_t)L->N * y_elem;
         if ((y_elem > 1 || L->N >= 32) && (rc = make_map_nhwc(&y_map, Y, rb, p.Q, p.P, Nb, 32, bx, by, 32))) return rc;
         if (y_elem > 1) y_map16 = y_map;
         else if ((rc = make_map_nhwc(&y_map16, Y, rb, p.Q, p.P, Nb, 16, bx, by, 0))) return rc;
-    } else if (staged && stream) {
+    } else if (mapped && stream) {
         // a warp's 32 accumulator rows are bx pixels of bi images of by rows
         const uint32_t pw = 1u << p.pw_log2, bx = pw < 32u ? pw : 32u, ni = 1u << p.img_log2, bi = ni < 32u / bx ? ni : 32u / bx, by = 32u / (bx * bi);
         const uint64_t rb = (uint64_t)L->N * y_elem;
         if ((y_elem > 1 || L->N >= 32) && (rc = make_map_nhwc_by_row(&y_map, Y, rb, p.Q, p.P, Nb, 32, bx, bi, by, 32))) return rc;
         if (y_elem > 1) y_map16 = y_map;
         else if ((rc = make_map_nhwc_by_row(&y_map16, Y, rb, p.Q, p.P, Nb, 16, bx, bi, by, 0))) return rc;
-    } else if (staged && y_elem > 1) {
+    } else if (mapped && y_elem > 1) {
         // rows of N 2- or 4-byte values addressed in bytes: a box is 32 bytes (16 or 8 columns) x 32 rows
         if ((rc = make_map_2d(&y_map, Y, (uint64_t)L->N * y_elem, (uint64_t)M, (uint64_t)L->N * y_elem, 32, 32, 32))) return rc;
         y_map16 = y_map;
-    } else if (staged) {
+    } else if (mapped) {
         if (L->N >= 32 && (rc = make_map_2d(&y_map, Y, (uint64_t)L->N, (uint64_t)M, (uint64_t)L->N, 32, 32, 32))) return rc;
         if ((rc = make_map_2d(&y_map16, Y, (uint64_t)L->N, (uint64_t)M, (uint64_t)L->N, 16, 32, 0))) return rc;
     }
     if (!packed && !cached) {
-        cm.slab = slab; cm.Y = staged ? Y : nullptr; cm.M = M; cm.Nb = Nb; cm.H = H; cm.W = W; cm.bk = p.BK; cm.im2col = (int)p.im2col + 2 * (int)patch + 4 * (int)stream;
-        cm.staged = staged; cm.y_elem = y_elem; cm.a = a_hi; cm.y = y_map; cm.y16 = y_map16;
+        cm.slab = slab; cm.Y = mapped ? Y : nullptr; cm.M = M; cm.Nb = Nb; cm.H = H; cm.W = W; cm.bk = p.BK; cm.im2col = (int)p.im2col + 2 * (int)patch + 4 * (int)stream;
+        cm.staged = mapped; cm.y_elem = y_elem; cm.a = a_hi; cm.y = y_map; cm.y16 = y_map16;
     }
     // Early weight loads (see the kernel) are safe once some launch on this handle has waited for whatever wrote the weights: this
     // call's does, so the next may.  A captured call waits only within its own graph, which as a whole starts behind what the
