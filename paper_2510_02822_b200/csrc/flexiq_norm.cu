@@ -4,8 +4,8 @@
 //
 // Bound by memory: every input byte is to be read once and every output byte written once.  Three ways, by what fits where:
 //   rows   one position per image (layer normalisation): a warp, or four, holds a group in registers
-//   held   an image's block of channels (whole groups, 128 bytes a position where that is enough) is held in the shared memory of a block, or of a
-//          cluster of up to eight, between the statistics and their use; the blocks of a cluster exchange their groups' statistics
+//   held   an image's block of channels (whole groups; norm_plan.h says how many) is held in the shared memory of a block, or of a
+//          cluster of up to four, between the statistics and their use; the blocks of a cluster exchange their groups' statistics
 //          through distributed shared memory
 //   twice  larger images: the statistics of pieces of an image go to scratch memory, and a second kernel reads the input again, in
 //          the reverse order, so that what the L2 cache still holds of it comes first
@@ -506,8 +506,8 @@ __global__ void __launch_bounds__(T, 1024 / T) group_norm_held_kernel(const Norm
     __shared__ float2 fin[kMaxGroups], inbox[kNormCluster][kMaxGroups];
     __shared__ uint64_t arrived;
     // The blocks of a cluster write their groups' moments into one another's shared memory.  First each has to know that the others have begun
-    // and their barriers stand: that is waited for below, while the data comes.  (Reading them from the others between two barriers
-    // of the cluster was FIGURES slower.)
+    // and their barriers stand: that is waited for below, while the data comes.  (Reading them from the others between two
+    // barriers of the cluster: 32 x 196 x 256 fp16 6.5 us, 5.3 so.)
     if (a.cluster_log) announce(&arrived, (unsigned)(a.gpb << a.cluster_log) * 8u);
     // block (image and rank in the cluster, channel block)
     const int rank = (int)(blockIdx.x & ((1u << a.cluster_log) - 1u));
@@ -778,39 +778,51 @@ __global__ void __launch_bounds__(kNormThreads, 3) group_norm_apply_kernel(const
     const long long p0 = part * a.cut_span, left = a.P - p0;
     const int mine = (int)(left < 0 ? 0 : left < a.cut_span ? left : a.cut_span);
     const Place who(a);
-    const int lane = threadIdx.x & 31;
+    const int cnt = who.count(a, mine);
+    // The first values are asked for at once: the statistics' kernel writes none of X, and every block of it had waited for what ran before when it
+    // let this one begin.
+    const size_t e = ((size_t)img * a.P + p0 + who.pl) * a.C + c0 + (size_t)who.col * VEC;
+    const char *from = static_cast<const char *>(a.X) + e * P::kBytes;
+    const size_t bytes = (size_t)a.lanes * a.C * P::kBytes;
+    PieceRing<DT, VEC, NV, kApplyDepth> ring(hold_bytes, from, bytes, a.cpt > 1 ? 0 : cnt);
     ptx::pdl_wait();
-    for (int g = threadIdx.x >> 5; g < a.gpb; g += (int)blockDim.x >> 5) {
-        const float2 *from = a.stats + ((size_t)img * a.groups + block * a.gpb + g) * a.joined;
-        float d = 0.f, M2 = 0.f, c = 0.f;
-        const long long span = a.span << a.cluster_log;        // positions of one of them
+    {
+        const long long span = a.span << a.cluster_log;        // positions of an entry
         const float all = (float)(a.P * a.cpg), each = (float)(span * a.cpg);
-        auto weight = [&](int i) {                             // values of piece i
+        // 8 to 32 lanes a group: as many as let the block take all its groups at once (a warp for each, one after another, was 2 us slower with 32)
+        int k = 8;
+        while (k < 32 && a.gpb * k * 2 <= kNormThreads) k *= 2;
+        const int r = threadIdx.x & (k - 1);
+        auto weight = [&](int i) {                             // values of entry i
             const long long rest = a.P - i * span;
             return rest >= span ? each : rest > 0 ? (float)(rest * a.cpg) : 0.f;
         };
-        for (int i = lane; i < a.joined; i += 32) d = __fmaf_rn(weight(i), from[i].x, d);
-        const float centre = __fdiv_rn(warp_sum(d), all);
-        for (int i = lane; i < a.joined; i += 32) {
-            const float2 s = from[i];
-            const float w = weight(i), q = s.x - centre, wq = w * q;
-            c += wq;
-            M2 += __fmaf_rn(wq, q, s.y);
+        for (int g0 = 0; g0 < a.gpb; g0 += kNormThreads / k) { // (all lanes stay: the sums need them)
+            const int g = g0 + (int)threadIdx.x / k;
+            const float2 *at = a.stats + ((size_t)img * a.groups + block * a.gpb + (g < a.gpb ? g : 0)) * a.joined;
+            float d = 0.f, M2 = 0.f, c = 0.f;
+#pragma unroll 8
+            for (int i = r; i < a.joined; i += k) d = __fmaf_rn(weight(i), at[i].x, d);
+            const float centre = __fdiv_rn(part_sum(d, k), all);
+#pragma unroll 8
+            for (int i = r; i < a.joined; i += k) {
+                const float2 s = at[i];
+                const float q = s.x - centre, wq = weight(i) * q;
+                c += wq;
+                M2 += __fmaf_rn(wq, q, s.y);
+            }
+            M2 = part_sum(M2, k);
+            c = part_sum(c, k);
+            if (r == 0 && g < a.gpb) fin[g] = make_float2(centre + __fdividef(c, all), deviation_inverse(M2, all, a.eps));
         }
-        M2 = warp_sum(M2);
-        c = warp_sum(c);
-        if (lane == 0) fin[g] = make_float2(centre + __fdividef(c, all), deviation_inverse(M2, all, a.eps));
     }
     __syncthreads();
     ptx::pdl_launch_dependents();
-    const int cnt = who.count(a, mine);
     if (cnt == 0) return;
     float2 stat[S];
     Affine<VEC, MANY> f;
     int ent = 0;
     column_stats<VEC, MANY>(a, a.cpt > 1 ? 0 : who.col, fin, stat);
-    const size_t e = ((size_t)img * a.P + p0 + who.pl) * a.C + c0 + (size_t)who.col * VEC;
-    const char *from = static_cast<const char *>(a.X) + e * P::kBytes;
     const int ob = out_bytes(a.out);
     if (a.cpt > 1) {
         for (int j = 0; j < cnt; ++j) {
@@ -830,8 +842,7 @@ __global__ void __launch_bounds__(kNormThreads, 3) group_norm_apply_kernel(const
     const int c = c0 + who.col * VEC;
     f.set(a, c, stat);
     char *to = static_cast<char *>(a.out.Y) + (e + slab_shift(a.out, c, &ent)) * ob;
-    const size_t bytes = (size_t)a.lanes * a.C * P::kBytes, far = (size_t)a.lanes * a.C * ob;
-    PieceRing<DT, VEC, NV, kApplyDepth> ring(hold_bytes, from, bytes, cnt);
+    const size_t far = (size_t)a.lanes * a.C * ob;
     auto batch = [&](auto whole, int n) {                  // (what is not there is not stored)
         ring.turn();
         pair_t x[NV][kPairs];
@@ -981,6 +992,16 @@ template <class K> static int allow_smem(K kernel, bool (&done)[64], int bytes)
     if (dev < 64) done[dev] = true;
     return FLEXIQ_OK;
 }
+// Blocks of clusters go to as few SMs as hold them, which leaves others idle.  Where the blocks are few, they ask for so much shared memory that no
+// SM takes more than its share: 32 x 784 x 256 fp16 in 32 groups 10.5 us, 11.9 without.  (One block to each SM only with an eighth of them to spare: a
+// part of the machine whose SMs the cluster's size does not divide leaves some free.)
+constexpr int kSmemSM = 228 * 1024;
+static int spread_smem(int need, long long blocks, int sms)
+{
+    const long long share = blocks * 8 <= sms * 7ll ? 1 : blocks <= 2ll * sms ? 2 : 3;
+    const int apart = kSmemSM / ((int)share + 1);
+    return share < 3 && need < apart ? apart : need;
+}
 static void set_attributes(cudaLaunchAttribute *attr, unsigned cluster)
 {
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -990,14 +1011,15 @@ static void set_attributes(cudaLaunchAttribute *attr, unsigned cluster)
     attr[1].val.clusterDim.y = 1;
     attr[1].val.clusterDim.z = 1;
 }
-template <int DT, int VEC, bool MANY, int T> static int launch_held_threads(const NormArgs &a, const NormPlan &p, cudaStream_t st)
+template <int DT, int VEC, bool MANY, int T> static int launch_held_threads(const NormArgs &a, const NormPlan &p, int sms, cudaStream_t st)
 {
     static bool done[64] = {};
-    if (int rc = allow_smem(group_norm_held_kernel<DT, VEC, MANY, T>, done, kNormHold)) return rc;
+    if (int rc = allow_smem(group_norm_held_kernel<DT, VEC, MANY, T>, done, kSmemSM / 2)) return rc;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(a.Nb << a.cluster_log), (unsigned)(a.groups / a.gpb), 1);
     cfg.blockDim = dim3((unsigned)T, 1, 1);
-    cfg.dynamicSmemBytes = (size_t)p.nv * T * (VEC == 1 ? 4 : 16);
+    const int need = p.nv * T * (VEC == 1 ? 4 : 16);
+    cfg.dynamicSmemBytes = a.cluster_log ? spread_smem(need, (long long)cfg.gridDim.x * cfg.gridDim.y, sms) : need;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     set_attributes(attr, 1u << a.cluster_log);
@@ -1006,13 +1028,13 @@ template <int DT, int VEC, bool MANY, int T> static int launch_held_threads(cons
     FLEXIQ_CUDA_TRY(cudaLaunchKernelEx(&cfg, group_norm_held_kernel<DT, VEC, MANY, T>, a));
     return FLEXIQ_OK;
 }
-template <int DT, int VEC, bool MANY> static int launch_held(const NormArgs &a, const NormPlan &p, cudaStream_t st)
+template <int DT, int VEC, bool MANY> static int launch_held(const NormArgs &a, const NormPlan &p, int sms, cudaStream_t st)
 {
     switch (p.threads) {
-        case 64: return launch_held_threads<DT, VEC, MANY, 64>(a, p, st);
-        case 128: return launch_held_threads<DT, VEC, MANY, 128>(a, p, st);
-        case 256: return launch_held_threads<DT, VEC, MANY, 256>(a, p, st);
-        default: return launch_held_threads<DT, VEC, MANY, 512>(a, p, st);
+        case 64: return launch_held_threads<DT, VEC, MANY, 64>(a, p, sms, st);
+        case 128: return launch_held_threads<DT, VEC, MANY, 128>(a, p, sms, st);
+        case 256: return launch_held_threads<DT, VEC, MANY, 256>(a, p, sms, st);
+        default: return launch_held_threads<DT, VEC, MANY, 512>(a, p, sms, st);
     }
 }
 template <int DT, int VEC, bool MANY> static int launch_twice(const NormArgs &a, const NormPlan &p, cudaStream_t st)
@@ -1076,7 +1098,7 @@ template <int DT> static int launch_norm(const NormArgs &a, const NormPlan &p, i
 {
     constexpr int V = FullVec<DT>::v;
     if (p.kind == kNormRows) return p.vec == 1 ? launch_norm_rows<DT, 1>(a, p, sms, st) : launch_norm_rows<DT, V>(a, p, sms, st);
-    if (p.kind == kNormHeld) return p.vec == 1 ? launch_held<DT, 1, false>(a, p, st) : p.many ? launch_held<DT, V, true>(a, p, st) : launch_held<DT, V, false>(a, p, st);
+    if (p.kind == kNormHeld) return p.vec == 1 ? launch_held<DT, 1, false>(a, p, sms, st) : p.many ? launch_held<DT, V, true>(a, p, sms, st) : launch_held<DT, V, false>(a, p, sms, st);
     return p.vec == 1 ? launch_twice<DT, 1, false>(a, p, st) : p.many ? launch_twice<DT, V, true>(a, p, st) : launch_twice<DT, V, false>(a, p, st);
 }
 

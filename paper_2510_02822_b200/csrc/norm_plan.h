@@ -7,8 +7,10 @@ namespace flexiq {
 constexpr int kNormThreads = 256;
 constexpr int kRowWarps = 4;           // warps that take a long row together
 constexpr int kNormHold = 65536;        // bytes a block holds ("held")
-constexpr int kNormCluster = 8;        // blocks of a cluster at most ("held")
-constexpr int kNormSplits = 512;       // pieces of an image's channel block at most ("twice")
+constexpr int kNormCluster = 4;        // blocks of a cluster at most ("held")
+constexpr int kNormEntries = 160;      // statistics of an image's group that "twice" leaves for its second kernel, at most
+constexpr int kNormSplits = 2 * kNormEntries;   // pieces of an image's channel block at most ("twice")
+constexpr int kNormCuts = 512;          // and for the second kernel
 constexpr int kMaxGroups = 128;        // groups of a channel block at most
 
 enum NormKind { kNormRows, kNormHeld, kNormTwice };
@@ -33,7 +35,7 @@ inline NormPlan plan_norm(int x_dtype, long long Nb, long long P, int C, int gro
             return p;
         }
     }
-    // the smallest block of whole groups and whole pieces, then more groups until a position's part is 128 bytes
+    // the smallest block of whole groups and whole pieces, then more groups
     const int base_groups = C % full == 0 ? full / gcd(cpg, full) : 1;
     const long long base_pieces = (long long)base_groups * cpg / full;
     p.vec = C % full == 0 && (base_pieces <= kNormThreads || cpg % full == 0) ? full : 1;
@@ -44,8 +46,12 @@ inline NormPlan plan_norm(int x_dtype, long long Nb, long long P, int C, int gro
         p.many = p.vec > 1 && cpg % p.vec != 0;
         p.cpt = (int)ceil_div(p.nch, kNormThreads);
     };
+    auto run = [&](int w) { return (long long)unit_groups * w * cpg * bytes; };   // bytes of a position that a block takes
+    // Runs of 128 bytes at least, and of short images so many channels that a block's own work (sums over its threads, the joining) is spread over
+    // 32 KB: 1024 x 49 x 512 fp16 in 32 groups 25.5 us, 40.7 in runs of 128 bytes; 4096 x 16 x 256 in 8 groups 21 and 31.
+    const bool one_wave = Nb * P * C * bytes <= 2ll * sms * kNormHold;
     int m = 1;
-    while (m < units && (long long)unit_groups * m * cpg * bytes < 128 && unit_groups * m < kMaxGroups / 2) {
+    while (m < units && (run(m) < 128 || run(m) * P < kNormHold / 2) && unit_groups * m < kMaxGroups / 2) {
         int next = m + 1;
         while (units % next) ++next;
         if ((long long)unit_groups * next * cpg / p.vec > kNormThreads || unit_groups * next > kMaxGroups) break;
@@ -57,6 +63,11 @@ inline NormPlan plan_norm(int x_dtype, long long Nb, long long P, int C, int gro
         // positions a block holds: 64 KB of pieces (two blocks an SM), eight a thread of 512 (a piece of the scalar form is shorter, but as long to work on)
         const long long capacity = p.cpt > 1 ? 16 / p.cpt : (long long)(512 / p.nch) * 8;
         if (capacity < 1 || ceil_div(P, capacity) > kNormCluster) continue;
+        // Narrow runs, or several blocks to an image, only where the machine holds all of it at once: beyond that the second read comes from the
+        // L2 cache and "twice" is faster (32 x 3136 x 256 fp16 in 32 groups 28 us, held 34; 8 x 4096 x 320 17.4 and 22.9).  Within it holding is
+        // (32 x 784 x 128 8.0 us, twice 11.5), from sectors of 32 bytes on (8 x 12544 x 64 in runs of 16 bytes 17.7 us, twice 14.6).
+        if (w < m && (run(w) < 32 || !one_wave)) continue;
+        if (ceil_div(P, capacity) > 1 && !one_wave) continue;
         p.kind = kNormHeld;
         p.threads = kNormThreads;
         const long long blocks = Nb * (units / w);
@@ -89,20 +100,21 @@ inline NormPlan plan_norm(int x_dtype, long long Nb, long long P, int C, int gro
     // Pieces: as many as make whole waves of the blocks that fit an SM (nine tenths of one at least, where up to four waves allow that), and a few
     // steps each.  Two blocks fit with the statistics' registers, three with those of the second kernel, which cuts the image anew.
     const long long blocks = Nb * (units / m), steps = p.cpt > 1 ? P : ceil_div(P, (long long)p.lanes * 8);
-    auto pieces = [&](long long wave) {
+    auto pieces = [&](long long wave, int most) {
         long long k = 1;
         for (long long w = 1; w <= 4; ++w) {
             k = w * wave / blocks;
             if (k * blocks * 10 >= w * wave * 9) break;
         }
         k = k < steps ? k : steps;
-        return (int)(k < 1 ? 1 : k < kNormSplits ? k : kNormSplits);
+        return (int)(k < 1 ? 1 : k < most ? k : most);
     };
-    p.cluster = pieces(2ll * sms);
-    p.cluster_log = p.cluster > 128 ? 2 : 0;   // the statistics of four pieces are joined where they are made (clusters of eight found no room: FIGURES)
+    p.cluster = pieces(2ll * sms, kNormSplits);
+    p.cluster_log = p.cluster > kNormEntries ? 1 : 0;   // the statistics of two pieces are joined where they are made
+    // (1 x 409600 x 128 fp16: 62.3 us, 66.0 with every piece's left to the second kernel, 66.6 with four joined, whose clusters found room on fewer SMs)
     p.cluster &= ~((1 << p.cluster_log) - 1);
     p.span = ceil_div(P, p.cluster);
-    p.cuts = pieces(3ll * sms);
+    p.cuts = pieces(3ll * sms, kNormCuts);
     p.cut_span = ceil_div(P, p.cuts);
     return p;
 }

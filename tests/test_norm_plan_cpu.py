@@ -30,7 +30,8 @@ static int check(int dt, long long Nb, long long P, int C, int groups)
     if (p.cpt > 1 && (p.gpb != 1 || p.many || p.threads != kNormThreads || p.lanes != 1 || p.cpt * p.threads < p.nch)) return bad("wide positions");
     if (p.cpt == 1 && (p.lanes < 1 || p.lanes * p.nch > p.threads)) return bad("lanes");
     if (p.cluster < 1 || p.cluster > (p.kind == kNormHeld ? kNormCluster : kNormSplits) || p.span * p.cluster < P || p.span < 1) return bad("pieces of an image");
-    if (p.kind == kNormTwice && (p.cuts < 1 || p.cuts > kNormSplits || p.cut_span * p.cuts < P || p.cut_span < 1)) return bad("the second kernel's pieces");
+    if (p.kind == kNormTwice && (p.cuts < 1 || p.cuts > kNormCuts || p.cut_span * p.cuts < P || p.cut_span < 1)) return bad("the second kernel's pieces");
+    if (p.kind == kNormTwice && p.cluster >> p.cluster_log > kNormEntries) return bad("statistics left for the second kernel");
     if (p.kind == kNormHeld) {
         if ((p.cluster & (p.cluster - 1)) || p.nv < 1 || p.nv * p.threads * 16 > kNormHold || (p.threads != 64 && p.threads != 128 && p.threads != 256 && p.threads != 512)) return bad("what a block holds");
         std::vector<unsigned char> seen((size_t)p.span * p.nch, 0);
