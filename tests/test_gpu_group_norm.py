@@ -73,7 +73,9 @@ def run(x, groups, gamma, beta, act, out, dev, eps=1e-5):
 SHAPES = [(1, 1, 16, 1), (3, 1, 768, 1), (197, 1, 384, 1), (5, 1, 1000, 4), (1, 1, 4096, 1), (70, 1, 17, 1), (2, 1, 9000, 2), (1, 1, 32, 32),
           (1, 49, 512, 32), (32, 49, 64, 32), (3, 9, 96, 32), (2, 100, 320, 32), (2, 81, 640, 32), (1, 1000, 48, 4), (7, 3, 30, 5), (2, 50, 33, 11),
           (1, 2, 77, 1), (4, 197, 768, 1), (2, 64, 2056, 8), (1, 60, 5000, 2), (3, 3136, 64, 32), (1, 4097, 128, 8), (2, 2, 64, 64), (9, 1023, 24, 2),
-          (1, 16384, 128, 32), (1, 70001, 16, 4), (2, 30000, 40, 8), (1, 40000, 12, 3), (1, 9001, 6, 2), (500, 4, 64, 8), (1, 300, 8224, 32)]
+          (1, 16384, 128, 32), (1, 70001, 16, 4), (2, 30000, 40, 8), (1, 40000, 12, 3), (1, 9001, 6, 2), (500, 4, 64, 8), (1, 300, 8224, 32),
+          (1, 66000, 128, 32), (1, 90001, 64, 1), (700, 49, 128, 32), (4100, 3, 192, 12), (40, 49, 2048, 32), (24, 784, 256, 32), (3, 900, 1280, 32), (2, 12544, 64, 32),
+          (40, 1024, 320, 32)]
 
 
 @pytest.mark.parametrize("Nb,P,C,groups", SHAPES)
@@ -268,6 +270,33 @@ def test_streams_and_graphs(dev):
         graphs[0].replay()
         torch.cuda.synchronize()
         assert torch.equal(held[0], fx.group_norm(xs[0][0], groups, xs[0][1], xs[0][2], act=fx.ACT_SILU))
+
+
+@pytest.mark.parametrize("Nb,P,C,groups", [(1, 66000, 128, 32), (3, 30000, 64, 8), (24, 784, 256, 32), (600, 49, 128, 32), (500, 1, 768, 1)])
+def test_calls_behind_one_another(dev, Nb, P, C, groups):
+    """Kernels that begin before the ones in front of them have ended: the input rewritten before each call, the output normalised again in
+    place, and nothing waited for in between, gives what a wait after every step gives."""
+    x, gamma, beta = draw((Nb, P, C), torch.float16, dev, seed=11)
+    other = torch.randn(Nb, P, C, device=dev).half()
+
+    def steps(after):
+        v, outs = x.clone(), []
+        for i in range(6):
+            v.add_(other, alpha=0.25)
+            after()
+            y = fx.group_norm(v, groups, gamma, beta, act=fx.ACT_SILU)
+            after()
+            fx.group_norm(y, groups, gamma, beta, Y=y)
+            after()
+            fx.group_norm(v, groups, None, beta, Y=v)
+            after()
+            outs.append(y)
+        return outs + [v]
+
+    want = steps(torch.cuda.synchronize)
+    got = steps(lambda: None)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
 def test_mlp_and_preactivation_chains(dev):
