@@ -277,7 +277,8 @@ int flexiq_mixed_conv_to_slab(flexiq_layer_t layer, const uint8_t *X4_dev, const
  * the quantized layers.  These calls do them where the data already is: in a layer's epilogue, and in one pass
  * from a floating-point tensor to a normalised one or to the next layer's slab.
  *
- * act: the activation function.  Evaluated in fp32; infinities give the functions' limits, NaNs stay NaN. */
+ * act: the activation function.  Evaluated in fp32: the error of act(v) is at most 2^-21 |v| (NONE and RELU are exact);
+ * infinities give the functions' limits, NaNs stay NaN. */
 #define FLEXIQ_ACT_NONE 0
 #define FLEXIQ_ACT_RELU 1      /* max(v, 0)                                                    */
 #define FLEXIQ_ACT_GELU 2      /* v Phi(v), Phi the normal distribution function               */
@@ -333,7 +334,9 @@ int flexiq_mixed_conv_act_to_slab(flexiq_layer_t layer, const uint8_t *X4_dev, c
  *   scratch_dev  device memory of the size flexiq_group_norm_scratch gives (16-byte aligned; NULL where that is
  *            0), written and read by this call's kernels: calls whose kernels may overlap need one each
  * C is any multiple of groups.  X_dev, Y_dev, gamma_dev and beta_dev 16-byte aligned.  Nb == 0 or P == 0 is a
- * successful no-op.  Enqueued on `stream` of the current device; nothing is allocated. */
+ * successful no-op; FLEXIQ_ERR_UNSUPPORTED beyond 2^30 blocks of images, or 65535 blocks of channels.  Enqueued on `stream` of the
+ * current device; nothing is allocated.  The same call gives the same bits; the order of an image's sums depends on the whole shape,
+ * Nb included, and on the device's number of SMs, so an image alone and the same image in a batch may differ in the last bits. */
 int flexiq_group_norm(const void *X_dev, int x_dtype, int64_t Nb, int64_t P, int C, int groups,
                       const float *gamma_dev, const float *beta_dev, float eps, int act, int y_dtype, void *Y_dev,
                       void *scratch_dev, void *stream);

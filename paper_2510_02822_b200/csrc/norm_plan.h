@@ -47,31 +47,35 @@ inline NormPlan plan_norm(int x_dtype, long long Nb, long long P, int C, int gro
         p.cpt = (int)ceil_div(p.nch, kNormThreads);
     };
     auto run = [&](int w) { return (long long)unit_groups * w * cpg * bytes; };   // bytes of a position that a block takes
+    // Positions a block holds: 64 KB of pieces (two blocks an SM), eight a thread of 512 (a piece of the scalar form is shorter, but as long to work on).
+    auto capacity = [&](int w) {
+        const long long nch = (long long)unit_groups * w * cpg / p.vec;
+        return nch > kNormThreads ? 16 / ceil_div(nch, kNormThreads) : 512 / nch * 8;
+    };
+    const bool one_wave = Nb * P * C * bytes <= 2ll * sms * kNormHold;
     // Runs of 128 bytes at least, and of short images so many channels that a block's own work (sums over its threads, the joining) is spread over
     // 32 KB: 1024 x 49 x 512 fp16 in 32 groups 25.5 us, 40.7 in runs of 128 bytes; 4096 x 16 x 256 in 8 groups 21 and 31.
-    const bool one_wave = Nb * P * C * bytes <= 2ll * sms * kNormHold;
     int m = 1;
     while (m < units && (run(m) < 128 || run(m) * P < kNormHold / 2) && unit_groups * m < kMaxGroups / 2) {
         int next = m + 1;
         while (units % next) ++next;
-        if ((long long)unit_groups * next * cpg / p.vec > kNormThreads || unit_groups * next > kMaxGroups) break;
+        if ((long long)unit_groups * next * cpg / p.vec > kNormThreads || unit_groups * next > kMaxGroups || (run(m) >= 128 && capacity(next) < P)) break;
         m = next;
     }
     for (int w = m; w >= 1; --w) {
         if (units % w) continue;
         shape(w);
-        // positions a block holds: 64 KB of pieces (two blocks an SM), eight a thread of 512 (a piece of the scalar form is shorter, but as long to work on)
-        const long long capacity = p.cpt > 1 ? 16 / p.cpt : (long long)(512 / p.nch) * 8;
-        if (capacity < 1 || ceil_div(P, capacity) > kNormCluster) continue;
+        const long long most = capacity(w);
+        if (most < 1 || ceil_div(P, most) > kNormCluster) continue;
         // Narrow runs, or several blocks to an image, only where the machine holds all of it at once: beyond that the second read comes from the
         // L2 cache and "twice" is faster (32 x 3136 x 256 fp16 in 32 groups 28 us, held 34; 8 x 4096 x 320 17.4 and 22.9).  Within it holding is
         // (32 x 784 x 128 8.0 us, twice 11.5), from sectors of 32 bytes on (8 x 12544 x 64 in runs of 16 bytes 17.7 us, twice 14.6).
         if (w < m && (run(w) < 32 || !one_wave)) continue;
-        if (ceil_div(P, capacity) > 1 && !one_wave) continue;
+        if (ceil_div(P, most) > 1 && !one_wave) continue;
         p.kind = kNormHeld;
         p.threads = kNormThreads;
         const long long blocks = Nb * (units / w);
-        int k = round_up_pow2(ceil_div(P, capacity));
+        int k = round_up_pow2(ceil_div(P, most));
         // more blocks where the machine has room for them and a thread more than one piece
         while (k < kNormCluster && blocks * k * 2 <= 2 * sms && ceil_div(P, k) > (p.cpt > 1 ? 1 : kNormThreads / p.nch)) k *= 2;
         p.cluster = k;
