@@ -159,6 +159,10 @@ template <int VEC, bool MANY> struct Affine {
     __device__ __forceinline__ void set(const NormArgs &n, int c, const float2 *stat)
     {
         load_affine<VEC>(n, c, scale, beta);
+        finish(stat);
+    }
+    __device__ __forceinline__ void finish(const float2 *stat)   // (what load_affine has put here goes with `stat`)
+    {
 #pragma unroll
         for (int i = 0; i < kPairs; ++i) scale[i] = mul2(scale[i], pair(stat[MANY ? 2 * i : 0].y, stat[MANY ? 2 * i + 1 : 0].y));
 #pragma unroll
@@ -572,6 +576,14 @@ __global__ void __launch_bounds__(T, 1024 / T) group_norm_held_kernel(const Norm
         }
         squares_of<VEC, MANY>(q, M2);
     }
+    // the channels' own numbers, asked for ahead of the exchange
+    Affine<VEC, MANY> f;
+    int ent = 0, shift = 0;
+    const int c_own = c0 + who.col * VEC;
+    if (!wide && cnt) {
+        load_affine<VEC>(a, c_own, f.scale, f.beta);
+        shift = slab_shift(a.out, c_own, &ent);
+    }
     put_moments<VEC, MANY, T>(a, who.col, mean, M2, (float)cnt, red_mean, red_M2, red_n);
     block_moments<VEC, MANY, T>(a, red_mean, red_M2, red_n, gstat);
     if (a.cluster_log) {
@@ -596,16 +608,13 @@ __global__ void __launch_bounds__(T, 1024 / T) group_norm_held_kernel(const Norm
     __syncthreads();
     if (cnt) {
         float2 stat[S];
-        Affine<VEC, MANY> f;
-        int ent = 0;
         const int ob = out_bytes(a.out);
         column_stats<VEC, MANY>(a, wide ? 0 : who.col, fin, stat);   // (wide: one group)
         const uint8_t *at = hold;
         if (!wide) {
             constexpr int NV = 2;
-            const int c = c0 + who.col * VEC;
-            f.set(a, c, stat);
-            char *to = static_cast<char *>(a.out.Y) + (e0 + slab_shift(a.out, c, &ent)) * ob;
+            f.finish(stat);
+            char *to = static_cast<char *>(a.out.Y) + (e0 + shift) * ob;
             const size_t far = step * ob;
             auto batch = [&](auto whole, int n) {              // (what is not there is not stored)
                 pair_t x[NV][kPairs];
