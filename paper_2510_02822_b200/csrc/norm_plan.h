@@ -54,7 +54,7 @@ inline NormPlan plan_norm(int x_dtype, long long Nb, long long P, int C, int gro
     };
     const bool one_wave = Nb * P * C * bytes <= 2ll * sms * kNormHold;
     // Runs of 128 bytes at least, and of short images so many channels that a block's own work (sums over its threads, the joining) is spread over
-    // 32 KB: 1024 x 49 x 512 fp16 in 32 groups 25.5 us, 40.7 in runs of 128 bytes; 4096 x 16 x 256 in 8 groups 21 and 31.
+    // 32 KB: 1024 x 49 x 512 fp16 in 32 groups 24.6 us, 40.7 in runs of 128 bytes; 4096 x 16 x 256 in 8 groups 21 and 31.
     int m = 1;
     while (m < units && (run(m) < 128 || run(m) * P < kNormHold / 2) && unit_groups * m < kMaxGroups / 2) {
         int next = m + 1;
