@@ -486,6 +486,7 @@ __device__ __forceinline__ void epilogue_role(const GemmParams &p, const Epilogu
     // to 5 % at 3072 (four stages 15 %, hence no more than 64 bytes of a row at a time).
     const int res_log = p.res_dtype == FLEXIQ_DTYPE_F32 ? 2 : 1;   // bytes of a value
     bool res_asked = false;                      // the first piece of the coming pass is under way
+    uint32_t scatter_half = 0;                   // where the next scattered chunk is staged
     auto request_residual = [&](long long r, int n) {
         if (n >= p.N) return;
 #pragma unroll
@@ -641,7 +642,8 @@ __device__ __forceinline__ void epilogue_role(const GemmParams &p, const Epilogu
                         const int ent_u = u == 0 ? ents[0] : u == 1 ? ents[1] : u == 2 ? ents[2] : ents[3];
                         uint32_t w[4];
                         quantize16_next(p, ent_u, v, w);
-                        const uint32_t half = x.store_stage + (uint32_t)(u & 1) * 512u;
+                        const uint32_t half = x.store_stage + scatter_half;
+                        scatter_half ^= 512u;                            // (by the store, not by the unit: the last tile of a row may have an odd number)
                         if (lane == 0) ptx::bulk_wait_read<1>();         // the store before the previous one has read its buffer
                         __syncwarp();
                         ptx::st_shared_128(half + (uint32_t)lane * 16u, w[0], w[1], w[2], w[3]);

@@ -143,6 +143,32 @@ def test_conv(dev, Nb, H, C, Cout, R, stride):
     L.close()
 
 
+@pytest.mark.parametrize("N", [16, 48, 272, 528, 560])
+def test_boundary_of_many_tiles_with_a_narrow_last_one(dev, N):
+    """An odd number of 16-channel chunks, so that a warp stages one chunk in one tile and the next chunk in the next: many tiles a block, hardly
+    any work between them, several times."""
+    rng = np.random.default_rng(N)
+    M, K = 24000, 64
+    A = fx.Layer(torch.from_numpy(rng.integers(-127, 128, (K, N)).astype(np.int8)).to(dev), torch.full((N,), 1e-3, device=dev), torch.randn(N, device=dev),
+                 rng.permutation(K // 16).astype(np.int32), rng.integers(0, 5, K // 16).astype(np.uint8), 16)
+    B = fx.Layer(torch.from_numpy(rng.integers(-127, 128, (N, 32)).astype(np.int8)).to(dev), torch.ones(32, device=dev), None,
+                 rng.permutation(N // 16).astype(np.int32), rng.integers(0, 5, N // 16).astype(np.uint8), 16)
+    for L in (A, B):
+        L.set_lowbit_ratio(0.5)
+    x4, x8, _ = A.quantize_lower(torch.randn(M, K, device=dev), 0.03)
+    for act in (fx.ACT_NONE, fx.ACT_SILU):
+        y = A.mixed_gemm_act(x4, x8, M, 0.03, act, fx.OUT_DEQUANT_F32)
+        two = B.quantize_lower(y, 0.02)[0][:M * N].view(torch.uint8).view(M, N).clone()
+        for _ in range(4):
+            slab, guard = helpers.with_guard(torch, (M, N), torch.uint8, dev)
+            A.mixed_gemm_act_to_slab(x4, x8, M, 0.03, B, 0.02, act, slab=slab)
+            torch.cuda.synchronize()
+            guard()
+            assert torch.equal(slab, two)
+    for L in (A, B):
+        L.close()
+
+
 @pytest.mark.parametrize("M,K,N1,G1,G2", [(300, 256, 272, 16, 16), (129, 128, 64, 16, 32), (1, 64, 16, 16, 16), (1000, 384, 1024, 16, 64), (260, 1280, 112, 16, 16)])
 def test_boundary_equals_the_two_calls(dev, M, K, N1, G1, G2):
     a = inputs.ranged_linear("a", M, K, N1, G1, seed=M, group_structured=True)
