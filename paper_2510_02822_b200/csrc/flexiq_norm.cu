@@ -11,8 +11,8 @@
 //          the reverse order, so that what the L2 cache still holds of it comes first
 //
 // Statistics.  The variance is a mean square of deviations, never a difference of two sums, which would lose everything where the mean
-// is large against the deviation.  A thread takes the mean and the sum of squared deviations M2 of its own values (at most 128, in registers, two
-// passes); those are joined in a fixed order by
+// is large against the deviation.  A thread takes the mean and the sum of squared deviations M2 of its own values (two passes over what it holds, 64
+// pieces at most; one about the first ones' mean where it holds nothing); those are joined in a fixed order by
 //   m = sum n_i mean_i / n,   q_i = mean_i - m,   mean = m + sum n_i q_i / n,   M2 = sum M2_i + n_i q_i^2
 // over the threads, the cluster's blocks or the pieces.  (The second sum takes out what the first has rounded.  The first is not taken from one of
 // the means: where that one holds an outlier, its rounding would be the error.)  No sum is longer than some sixty roundings, and results do not depend on timing.
@@ -29,7 +29,6 @@
 #include "norm_plan.h"
 
 namespace flexiq {
-
 
 // Where the results go: Y, or the slab of a layer.
 struct NormOut {
