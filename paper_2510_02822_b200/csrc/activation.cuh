@@ -142,13 +142,5 @@ template <int N> __device__ __forceinline__ void activate_n(int act, pair_t *v)
         default: break;
     }
 }
-__device__ __forceinline__ float activate_one(int act, float v)
-{
-    pair_t p = pair(v, v);
-    activate_n<1>(act, &p);
-    float b;
-    unpair(p, &v, &b);
-    return v;
-}
 
 }  // namespace flexiq
