@@ -765,7 +765,8 @@ __global__ void __launch_bounds__(kNormThreads, 2) group_norm_stats_kernel(const
         for (int g0 = 0; g0 < a.gpb; g0 += per) {              // (all lanes stay: the sums need them)
             const int g = g0 + (int)(threadIdx.x >> a.cluster_log);
             const Moments m = join_cluster(inbox[r][g < a.gpb ? g : 0], n, all, k);
-            if (r == 0 && g < a.gpb) to[(size_t)g * a.joined] = make_float2(m.mean, m.M2);
+            // (nothing to be joined, which no plan asks for, would be 0 / 0, a NaN that the entry's weight of zero does not take away)
+            if (r == 0 && g < a.gpb) to[(size_t)g * a.joined] = all > 0.f ? make_float2(m.mean, m.M2) : make_float2(0.f, 0.f);
         }
     } else {
         for (int g = threadIdx.x; g < a.gpb; g += kNormThreads) to[(size_t)g * a.joined] = make_float2(gstat[g].mean, gstat[g].M2);

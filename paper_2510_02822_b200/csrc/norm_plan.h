@@ -116,10 +116,15 @@ inline NormPlan plan_norm(int x_dtype, long long Nb, long long P, int C, int gro
     p.cluster = pieces(2ll * sms, kNormSplits);
     p.cluster_log = p.cluster > kNormEntries ? 1 : 0;   // the statistics of two pieces are joined where they are made
     // (1 x 409600 x 128 fp16: 62.3 us, 66.0 with every piece's left to the second kernel, 66.6 with four joined, whose clusters found room on fewer SMs)
-    p.cluster &= ~((1 << p.cluster_log) - 1);
+    // The positions of a piece are rounded up, so that fewer pieces than planned may hold them all: none is made without a position, but for the second
+    // of the last two where those are joined.
+    const int joined = 1 << p.cluster_log;
+    p.cluster &= ~(joined - 1);
     p.span = ceil_div(P, p.cluster);
+    p.cluster = ((int)ceil_div(P, p.span) + joined - 1) & ~(joined - 1);
     p.cuts = pieces(3ll * sms, kNormCuts);
     p.cut_span = ceil_div(P, p.cuts);
+    p.cuts = (int)ceil_div(P, p.cut_span);
     return p;
 }
 

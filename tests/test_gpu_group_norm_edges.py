@@ -1,0 +1,45 @@
+"""Group normalisation where an image's pieces end with the image.
+
+Tolerances as in test_gpu_group_norm."""
+import numpy as np
+import pytest
+import torch
+
+import helpers
+from paper_2510_02822_b200 import binding as fx
+from test_gpu_group_norm import check, draw, run, want_and_tolerance
+
+pytestmark = pytest.mark.gpu
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+
+
+@pytest.fixture(scope="module")
+def dev():
+    return torch.device("cuda:0")
+
+
+# On 148 SMs these images are cut in more pieces than their positions fill, the last full pair of them ending with the image.
+@pytest.mark.parametrize("P,C,groups,t", [(6600, 512, 4, F16), (8712, 512, 32, BF16), (10920, 256, 32, F16), (9800, 320, 32, F16), (9604, 320, 32, BF16), (4000, 640, 1, F16),
+                                          (6724, 192, 32, F32), (10270, 128, 32, F32), (33282, 128, 32, F16), (984, 435, 1, F16), (21316, 256, 32, F16)])
+def test_pieces_that_end_with_the_image(dev, P, C, groups, t):
+    x, gamma, beta = draw((1, P, C), t, dev, seed=P)
+    run(x, groups, gamma, beta, fx.ACT_SILU, t, dev)
+    y = run(x, groups, gamma, beta, fx.ACT_NONE, F32, dev)
+    mine = x.clone()
+    fx.group_norm(mine, groups, gamma, beta, act=fx.ACT_SILU, Y=mine)
+    assert torch.equal(mine, fx.group_norm(x, groups, gamma, beta, act=fx.ACT_SILU))
+    if C % 16 == 0:
+        L = fx.Layer(torch.zeros(C, 16, dtype=torch.int8, device=dev), torch.ones(16, device=dev), None, np.arange(C // 16, dtype=np.int32), np.full(C // 16, 2, np.uint8), 16)
+        L.set_lowbit_ratio(0.5)
+        two = L.quantize_lower(y, 0.02)[0][:P * C].clone()
+        assert torch.equal(L.group_norm_to_slab(x, groups, gamma, beta, 0.02, slab=torch.empty(P * C, dtype=torch.uint8, device=dev)), two)
+        L.close()
+
+
+def test_every_length_of_an_image(dev):
+    """One image of every length around the cuts, scalar and wide, by its sum of squares: NaN anywhere would show."""
+    for C, groups, t, lengths in ((512, 32, F16, range(6500, 6720, 7)), (128, 1, F32, range(10200, 10360, 5)), (435, 1, F16, range(900, 1060, 4))):
+        x, _, _ = draw((1, max(lengths), C), t, dev, seed=C)
+        for P in lengths:
+            y = fx.group_norm(x[:, :P], groups, out_dtype=F32)
+            assert abs(float(y.double().square().mean()) - 1) < 1e-4
