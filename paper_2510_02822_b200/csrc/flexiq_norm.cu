@@ -12,10 +12,11 @@
 //
 // Statistics.  The variance is a mean square of deviations, never a difference of two sums, which would lose everything where the mean
 // is large against the deviation.  A thread takes the mean and the sum of squared deviations M2 of its own values (two passes over what it holds, 64
-// pieces at most; one about the first ones' mean where it holds nothing); those are joined in a fixed order by
+// pieces at most; one about the first ones' mean where it holds nothing, 256 pieces at a time); those are joined in a fixed order by
 //   m = sum n_i mean_i / n,   q_i = mean_i - m,   mean = m + sum n_i q_i / n,   M2 = sum M2_i + n_i q_i^2
 // over the threads, the cluster's blocks or the pieces.  (The second sum takes out what the first has rounded.  The first is not taken from one of
-// the means: where that one holds an outlier, its rounding would be the error.)  No sum is longer than some sixty roundings, and results do not depend on timing.
+// the means: where that one holds an outlier, its rounding would be the error.)  No sum is longer than some sixty roundings, and
+// one more for every 256 pieces that a thread of "twice" has; results do not depend on timing.
 #include "flexiq_internal.h"
 
 #include <cuda_bf16.h>
@@ -649,6 +650,7 @@ __global__ void __launch_bounds__(T, 1024 / T) group_norm_held_kernel(const Norm
 }
 
 constexpr int kStatsPieces = 8, kStatsDepth = 2, kApplyPieces = 4, kApplyDepth = 3;
+constexpr int kStatsRun = 32;     // batches whose sums are taken about one K
 // "twice", the first: moments of a piece of an image's channel block
 template <int DT, int VEC, bool MANY>
 __global__ void __launch_bounds__(kNormThreads, 2) group_norm_stats_kernel(const NormArgs a)
@@ -672,17 +674,55 @@ __global__ void __launch_bounds__(kNormThreads, 2) group_norm_stats_kernel(const
     const int cnt = who.count(a, mine);
     const size_t step = (size_t)a.lanes * a.C * P::kBytes;
     ptx::pdl_wait();
-    // One pass: sums of x - K and of its square, K the mean of the thread's first pieces (of each channel: MANY).  Their squares' sum is at most
-    // 1 + n / NV^2 times what is left of it when the mean is taken out, however far one of the first values lies, since that one is among them; NV
-    // n pieces are summed apart before they are added to the rest, so no sum has more than some sixty roundings.
+    // One pass: sums of x - K and of its square, K the mean of the first NV pieces of a run of kStatsRun batches.  Their squares' sum is at most
+    // 1 + n / NV^2 = 5 times (n pieces) what is left of it when the mean is taken out, however far one of the first values lies, since that one is
+    // among them; four batches are summed apart before they are added to the rest of the run.  A run that more pieces follow is closed: its moments
+    // join those of the runs before it, which lie in the thread's own places of the block's arrays.  (One K for all of a thread's pieces, 4096 of
+    // them with an outlier in front: the variance off by 420 units of 2^-24, 5 so; none of the measured shapes has a second run.)
     const char *from = static_cast<const char *>(a.X) + e0 * P::kBytes;
     pair_t K[MANY ? kPairs : 1], S1[kPairs] = {}, S2[kPairs] = {};
     float shift[S] = {};
-    bool first = true;
     int batches = 0;
     pair_t s[kPairs] = {}, q[kPairs] = {};
+    const int own = threadIdx.x;
+    // the open run's moments, of `pieces`; those together with the closed runs'
+    auto run_moments = [&](int pieces, float *mean, float *M2) {
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) { S1[i] = add2(S1[i], s[i]); S2[i] = add2(S2[i], q[i]); }
+        float off[S];
+        means_of<VEC, MANY>(S1, pieces, off);
+        squares_of<VEC, MANY>(S2, M2);
+        const float n = (float)(pieces * (MANY ? 1 : VEC));
+#pragma unroll
+        for (int i = 0; i < S; ++i) {
+            mean[i] = shift[i] + off[i];
+            M2[i] = fmaxf(__fmaf_rn(-n * off[i], off[i], M2[i]), 0.f);   // (a NaN: see below)
+            if (off[i] != off[i]) M2[i] = off[i];
+        }
+    };
+    auto join_runs = [&](int pieces, float *mean, float *M2) {
+        const float before = red_n[own], part = __fdividef((float)pieces, before + (float)pieces), n = before * part * (MANY ? 1.f : (float)VEC);
+#pragma unroll
+        for (int i = 0; i < S; ++i) {
+            const float d = mean[i] - red_mean[i * kNormThreads + own];
+            mean[i] = __fmaf_rn(d, part, red_mean[i * kNormThreads + own]);
+            M2[i] = __fmaf_rn(d * n, d, M2[i] + red_M2[i * kNormThreads + own]);
+        }
+    };
+    auto close_run = [&] {
+        constexpr int kPieces = kStatsRun * NV;
+        float mean[S], M2[S];
+        run_moments(kPieces, mean, M2);
+        if (batches > kStatsRun) join_runs(kPieces, mean, M2);
+#pragma unroll
+        for (int i = 0; i < S; ++i) { red_mean[i * kNormThreads + own] = mean[i]; red_M2[i * kNormThreads + own] = M2[i]; }
+        red_n[own] = (float)(batches * NV);
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) S1[i] = S2[i] = s[i] = q[i] = pair(0.f, 0.f);
+    };
     auto tile = [&](auto piece, int pieces, auto all) {      // `all`: every piece of the tile is there
-        if (first) {
+        if (batches % kStatsRun == 0) {
+            if (batches) close_run();
             pair_t t[kPairs] = {};
 #pragma unroll
             for (int j = 0; j < NV; ++j)
@@ -694,7 +734,6 @@ __global__ void __launch_bounds__(kNormThreads, 2) group_norm_stats_kernel(const
                 }
             means_of<VEC, MANY>(t, pieces, shift);
             minus_means<VEC, MANY>(shift, K);
-            first = false;
         }
 #pragma unroll
         for (int j = 0; j < NV; ++j)
@@ -735,18 +774,9 @@ __global__ void __launch_bounds__(kNormThreads, 2) group_norm_stats_kernel(const
     }
     float mean[S], M2[S];
     {
-#pragma unroll
-        for (int i = 0; i < kPairs; ++i) { S1[i] = add2(S1[i], s[i]); S2[i] = add2(S2[i], q[i]); }
-        float off[S];
-        means_of<VEC, MANY>(S1, cnt, off);
-        squares_of<VEC, MANY>(S2, M2);
-        const float n = (float)(cnt * (MANY ? 1 : VEC));
-#pragma unroll
-        for (int i = 0; i < S; ++i) {
-            mean[i] = shift[i] + off[i];
-            M2[i] = fmaxf(__fmaf_rn(-n * off[i], off[i], M2[i]), 0.f);   // (a NaN: see below)
-            if (off[i] != off[i]) M2[i] = off[i];
-        }
+        const int closed = cnt ? (batches - 1) / kStatsRun * (kStatsRun * NV) : 0;   // pieces
+        run_moments(cnt - closed, mean, M2);
+        if (closed) join_runs(cnt - closed, mean, M2);
     }
     ptx::pdl_launch_dependents();
     put_moments<VEC, MANY, kNormThreads>(a, who.col, mean, M2, (float)cnt, red_mean, red_M2, red_n);

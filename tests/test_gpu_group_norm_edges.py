@@ -1,4 +1,4 @@
-"""Group normalisation where an image's pieces end with the image.
+"""Group normalisation where an image's pieces end with the image, and where a thread has thousands of them.
 
 Tolerances as in test_gpu_group_norm."""
 import numpy as np
@@ -43,3 +43,13 @@ def test_every_length_of_an_image(dev):
         for P in lengths:
             y = fx.group_norm(x[:, :P], groups, out_dtype=F32)
             assert abs(float(y.double().square().mean()) - 1) < 1e-4
+
+
+@pytest.mark.parametrize("P,C,groups,t", [(65539, 64, 32, F32), (131075, 64, 8, BF16), (65539, 64, 4, F32)])
+def test_an_outlier_in_front_of_a_long_image(dev, P, C, groups, t):
+    """Thousands of values a thread, the first of them far from all others: as many images as let a block take a whole one."""
+    x = torch.randn(296, P, C, device=dev, dtype=t)
+    x[:, 0, ::C // groups] = 30000.0
+    y = fx.group_norm(x, groups, out_dtype=t)
+    for i in (0, 100, 295):
+        check(y[i:i + 1], *want_and_tolerance(x[i:i + 1], groups, None, None, 1e-5, fx.ACT_NONE))
