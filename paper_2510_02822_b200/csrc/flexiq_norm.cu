@@ -1031,16 +1031,6 @@ template <class K> static int allow_smem(K kernel, bool (&done)[64], int bytes)
     if (dev < 64) done[dev] = true;
     return FLEXIQ_OK;
 }
-// Blocks of clusters go to as few SMs as hold them, which leaves others idle.  Where the blocks are few, they ask for so much shared memory that no
-// SM takes more than its share: 32 x 784 x 256 fp16 in 32 groups 10.5 us, 11.9 without.  (One block to each SM only with an eighth of them to spare: a
-// part of the machine whose SMs the cluster's size does not divide leaves some free.)
-constexpr int kSmemSM = 228 * 1024;
-static int spread_smem(int need, long long blocks, int sms)
-{
-    const long long share = blocks * 8 <= sms * 7ll ? 1 : blocks <= 2ll * sms ? 2 : 3;
-    const int apart = kSmemSM / ((int)share + 1);
-    return share < 3 && need < apart ? apart : need;
-}
 static void set_attributes(cudaLaunchAttribute *attr, unsigned cluster)
 {
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -1050,6 +1040,38 @@ static void set_attributes(cudaLaunchAttribute *attr, unsigned cluster)
     attr[1].val.clusterDim.y = 1;
     attr[1].val.clusterDim.z = 1;
 }
+// Clusters go to as few SMs as hold their blocks, which leaves others idle.  Where the machine has room for all of them with one block to an SM, or with two,
+// they ask for so much shared memory that no SM takes more: fp16, 32 groups, 32 x 784 x 256 (32 clusters of four) 8.6 us, 9.3 without; 33 x 1000 x 64 in 16
+// groups 7.0 and 8.5.  The room is asked for, since parts of the machine whose SMs the cluster's size does not divide leave some free: one cluster
+// more than there is room for waits for another's end (36 x 1053 x 64, 36 of them, 14.1 us so and 10.2 with two blocks to an SM).
+template <class K> static int spread_clusters(K kernel, cudaLaunchConfig_t &cfg, int cluster_log)
+{
+    struct Room { int own; int clusters[2][2]; };            // [log of the size - 1][blocks to an SM - 1], 0: not asked yet
+    static Room rooms[64] = {};                              // (per kernel and device; written twice at worst)
+    int dev = 0;
+    cudaGetDevice(&dev);
+    if (dev >= 64) return FLEXIQ_OK;
+    Room &room = rooms[dev];
+    const long long clusters = (long long)cfg.gridDim.x * cfg.gridDim.y >> cluster_log;
+    for (int share = 1; share <= 2; ++share) {
+        int &most = room.clusters[cluster_log - 1][share - 1];
+        if (!most) {
+            cudaFuncAttributes f;
+            FLEXIQ_CUDA_TRY(cudaFuncGetAttributes(&f, kernel));
+            room.own = (int)f.sharedSizeBytes;
+            cudaLaunchConfig_t ask = cfg;
+            ask.dynamicSmemBytes = apart_smem(share, room.own);
+            FLEXIQ_CUDA_TRY(cudaOccupancyMaxActiveClusters(&most, kernel, &ask));
+        }
+        const int apart = apart_smem(share, room.own);
+        if ((int)cfg.dynamicSmemBytes >= apart) return FLEXIQ_OK;
+        if (clusters <= most) {
+            cfg.dynamicSmemBytes = apart;
+            return FLEXIQ_OK;
+        }
+    }
+    return FLEXIQ_OK;
+}
 template <int DT, int VEC, bool MANY, int T> static int launch_held_threads(const NormArgs &a, const NormPlan &p, int sms, cudaStream_t st)
 {
     static bool done[64] = {};
@@ -1057,13 +1079,14 @@ template <int DT, int VEC, bool MANY, int T> static int launch_held_threads(cons
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(a.Nb << a.cluster_log), (unsigned)(a.groups / a.gpb), 1);
     cfg.blockDim = dim3((unsigned)T, 1, 1);
-    const int need = p.nv * T * (VEC == 1 ? 4 : 16);
-    cfg.dynamicSmemBytes = a.cluster_log ? spread_smem(need, (long long)cfg.gridDim.x * cfg.gridDim.y, sms) : need;
+    cfg.dynamicSmemBytes = p.nv * T * (VEC == 1 ? 4 : 16);
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     set_attributes(attr, 1u << a.cluster_log);
     cfg.attrs = attr;
     cfg.numAttrs = a.cluster_log ? 2 : 1;
+    if (a.cluster_log)
+        if (int rc = spread_clusters(group_norm_held_kernel<DT, VEC, MANY, T>, cfg, a.cluster_log)) return rc;
     FLEXIQ_CUDA_TRY(cudaLaunchKernelEx(&cfg, group_norm_held_kernel<DT, VEC, MANY, T>, a));
     return FLEXIQ_OK;
 }

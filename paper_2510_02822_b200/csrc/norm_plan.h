@@ -128,4 +128,9 @@ inline NormPlan plan_norm(int x_dtype, long long Nb, long long P, int C, int gro
     return p;
 }
 
+// The least dynamic shared memory with which an SM takes no more than `share` blocks that have `own` bytes of static arrays besides, and kSmemBlock of the
+// system's.
+constexpr int kSmemSM = 228 * 1024, kSmemBlock = 1024;
+inline int apart_smem(int share, int own) { return (kSmemSM / (share + 1) / 128 + 1) * 128 - kSmemBlock - own; }
+
 }  // namespace flexiq

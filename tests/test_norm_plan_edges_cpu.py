@@ -1,4 +1,4 @@
-"""How a group normalisation is cut up where an image's pieces end with the image."""
+"""How a group normalisation is cut up where an image's pieces end with the image, and how its clusters are spread over the SMs."""
 import os
 import subprocess
 
@@ -56,3 +56,28 @@ def run_plan(tmp_path, source):
 
 def test_no_piece_without_a_position(tmp_path):
     run_plan(tmp_path, PIECES)
+
+
+SPREAD = r"""
+#include "norm_plan.h"
+#include <stdio.h>
+using namespace flexiq;
+int main()
+{
+    int bad = 0;
+    for (int own = 512; own <= 48 * 1024; own += 512)             // static arrays: up to some 42 KB (512 threads, pieces of several groups)
+        for (int share = 1; share <= 2; ++share) {
+            const int bytes = apart_smem(share, own), block = bytes + own + 1024;
+            if (share * block > 228 * 1024 || (share + 1) * block <= 228 * 1024 || bytes + own > 227 * 1024 || bytes > kSmemSM / 2 || bytes < 0) {
+                printf("own %d, %d blocks an SM: %d\n", own, share, bytes);
+                ++bad;
+            }
+        }
+    return bad != 0;
+}
+"""
+
+
+def test_blocks_apart_but_not_further(tmp_path):
+    """So much shared memory that as many blocks as are meant share an SM, no more and no fewer."""
+    run_plan(tmp_path, SPREAD)
