@@ -298,7 +298,7 @@ int flexiq_mixed_conv_to_slab(flexiq_layer_t layer, const uint8_t *X4_dev, const
  *   residual_dev   row-major in the output's shape ([M][N], or [Nb][P][Q][Cout]), 16-byte aligned, or NULL for
  *                  none; residual_dtype F32, F16 or BF16, whatever the output's type
  *   Y_dev          may be residual_dev itself when both have the same type (the residual stream updated in
- *                  place); any other overlap of the two is not allowed.  FLEXIQ_OUT_ACC_I32 is refused.
+ *                  place); any other overlap of the two is refused, and so is FLEXIQ_OUT_ACC_I32.
  * Otherwise as flexiq_mixed_gemm / flexiq_mixed_conv. */
 int flexiq_mixed_gemm_act(flexiq_layer_t layer, const uint8_t *X4_dev, const int8_t *X8_dev,
                           const uint8_t *x_shift_dev, int64_t M, float x_scale, float y_scale, int act,
@@ -330,7 +330,8 @@ int flexiq_mixed_conv_act_to_slab(flexiq_layer_t layer, const uint8_t *X4_dev, c
  *   X_dev    [Nb][P][C], x_dtype F32, F16 or BF16
  *   gamma_dev, beta_dev  [C] fp32, or NULL (1 and 0)
  *   eps      positive
- *   Y_dev    [Nb][P][C], y_dtype F32, F16 or BF16; may be X_dev itself when the types are the same
+ *   Y_dev    [Nb][P][C], y_dtype F32, F16 or BF16; may be X_dev itself when the types are the same; any other overlap
+ *            of the two is refused
  *   scratch_dev  device memory of the size flexiq_group_norm_scratch gives (16-byte aligned; NULL where that is
  *            0), written and read by this call's kernels: calls whose kernels may overlap need one each
  * C is any multiple of groups.  X_dev, Y_dev, gamma_dev and beta_dev 16-byte aligned.  Nb == 0 or P == 0 is a
@@ -347,7 +348,7 @@ int flexiq_group_norm_scratch(int x_dtype, int64_t Nb, int64_t P, int C, int gro
  * what flexiq_group_norm(..., y_dtype F32) and flexiq_quantize_lower(layer, ., FLEXIQ_DTYPE_F32, Nb * P, x_scale,
  * static positions) compute, bit for bit, in one pass over X_dev.
  *   layer    on the MASKED path; its ratio at the time of this call decides the lowering
- *   X4_dev   [Nb * P][C] the layer's slab, 16-byte aligned */
+ *   X4_dev   [Nb * P][C] the layer's slab, 16-byte aligned, apart from X_dev */
 int flexiq_group_norm_to_slab(flexiq_layer_t layer, const void *X_dev, int x_dtype, int64_t Nb, int64_t P, int groups,
                               const float *gamma_dev, const float *beta_dev, float eps, int act, float x_scale,
                               uint8_t *X4_dev, void *scratch_dev, void *stream);

@@ -1994,6 +1994,9 @@ static int run_mixed(Layer *L, const uint8_t *X4, const int8_t *X8, const uint8_
                            : out_mode == FLEXIQ_OUT_DEQUANT_BF16 ? FLEXIQ_DTYPE_BF16 : -1;
             if (ops->res == Y && ops->res_dtype != same)
                 return set_error(FLEXIQ_ERR_INVALID_ARG, "Y_dev is residual_dev, which needs an output of the residual's type");
+            const long long values = M * L->N, out_bytes = out_mode == FLEXIQ_OUT_REQUANT_I8 ? 1 : out_mode == FLEXIQ_OUT_DEQUANT_F32 ? 4 : 2;
+            if (M && Y && ops->res != Y && share_memory(ops->res, values * (ops->res_dtype == FLEXIQ_DTYPE_F32 ? 4 : 2), Y, values * out_bytes))
+                return set_error(FLEXIQ_ERR_INVALID_ARG, "residual_dev and Y_dev overlap and are not the same");
         }
     }
     if (M == 0) return FLEXIQ_OK;

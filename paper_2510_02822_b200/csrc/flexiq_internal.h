@@ -146,6 +146,13 @@ int make_map_2d(CUtensorMap *map, const void *base, uint64_t row_bytes, uint64_t
 unsigned prologue_status();
 unsigned norm_status();   // the same of the group normalisation's
 
+// whether two pieces of memory share a byte
+inline bool share_memory(const void *a, long long a_bytes, const void *b, long long b_bytes)
+{
+    const uintptr_t p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
+    return p < q + (uintptr_t)b_bytes && q < p + (uintptr_t)a_bytes;
+}
+
 int choose_bk(const Layer *L);
 int encode_weight_maps(Layer *L);
 

@@ -1173,6 +1173,7 @@ unsigned norm_status()
     return word;
 }
 
+static long long value_bytes(int dtype) { return dtype == FLEXIQ_DTYPE_F32 ? 4 : 2; }
 static int check_shape(int x_dtype, int64_t Nb, int64_t P, int C, int groups)
 {
     if (x_dtype != FLEXIQ_DTYPE_F32 && x_dtype != FLEXIQ_DTYPE_F16 && x_dtype != FLEXIQ_DTYPE_BF16)
@@ -1246,8 +1247,10 @@ extern "C" int flexiq_group_norm(const void *X_dev, int x_dtype, int64_t Nb, int
         return set_error(FLEXIQ_ERR_INVALID_ARG, "y_dtype %d is not F32, F16 or BF16", y_dtype);
     int rc = check_norm(X_dev, x_dtype, Nb, P, C, groups, gamma_dev, beta_dev, eps, act, Y_dev);
     if (rc) return rc;
-    if (X_dev == Y_dev && x_dtype != y_dtype && Nb && P) return set_error(FLEXIQ_ERR_INVALID_ARG, "Y_dev is X_dev, which needs the same type");
     if (Nb == 0 || P == 0) return FLEXIQ_OK;
+    if (X_dev == Y_dev && x_dtype != y_dtype) return set_error(FLEXIQ_ERR_INVALID_ARG, "Y_dev is X_dev, which needs the same type");
+    if (X_dev != Y_dev && share_memory(X_dev, Nb * P * C * value_bytes(x_dtype), Y_dev, Nb * P * C * value_bytes(y_dtype)))
+        return set_error(FLEXIQ_ERR_INVALID_ARG, "X_dev and Y_dev overlap and are not the same");
     if ((rc = check_device_sm100())) return rc;
     NormArgs a{};
     a.X = X_dev; a.Nb = Nb; a.P = P; a.C = C; a.groups = groups; a.act = act;
@@ -1267,7 +1270,7 @@ extern "C" int flexiq_group_norm_to_slab(flexiq_layer_t layer, const void *X_dev
     int rc = check_norm(X_dev, x_dtype, Nb, P, L->C, groups, gamma_dev, beta_dev, eps, act, X4_dev);
     if (rc) return rc;
     if (Nb == 0 || P == 0) return FLEXIQ_OK;
-    if (static_cast<const void *>(X4_dev) == X_dev) return set_error(FLEXIQ_ERR_INVALID_ARG, "the slab cannot be X_dev");
+    if (share_memory(X_dev, Nb * P * L->C * value_bytes(x_dtype), X4_dev, Nb * P * L->C)) return set_error(FLEXIQ_ERR_INVALID_ARG, "X_dev and the slab overlap");
     if ((rc = check_device_sm100())) return rc;
     if ((rc = check_layer_device(L))) return rc;
     NormArgs a{};
