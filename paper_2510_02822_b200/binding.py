@@ -371,6 +371,12 @@ def _refuse(ok, message):
         raise FlexiqError(ERR_INVALID_ARG, message)
 
 
+def _refuse_long(**values):
+    """ctypes would cut off what does not fit the library's 32-bit arguments."""
+    for what, v in values.items():
+        _refuse(-2 ** 31 <= v < 2 ** 31, f"{what} = {v} does not fit 32 bits")
+
+
 def _check_tensor(t, what, numel, device, dtypes):
     """What the library takes as it is: a contiguous tensor on `device`, of this many elements and one of these types."""
     _refuse(t.is_cuda and t.device == device and t.is_contiguous() and t.numel() == numel and t.dtype in dtypes,
@@ -405,6 +411,7 @@ def _norm_args(X, gamma, beta):
     import torch
     _refuse(X.dim() >= 2 and X.is_cuda and X.is_contiguous() and X.dtype in _float_types(),
             "X must be a contiguous channels-last tensor [images, ..., channels] on a CUDA device, of type float32, float16 or bfloat16")
+    _refuse_long(channels=X.shape[-1])
     _refuse(X.device.index == torch.cuda.current_device(), f"X lies on {X.device}, which is not the current device")
     for t, what in ((gamma, "gamma"), (beta, "beta")):
         if t is not None:
@@ -431,6 +438,7 @@ def group_norm(X, groups, gamma=None, beta=None, eps=1e-5, act=ACT_NONE, out_dty
         if r is not NotImplemented:
             return r
     import torch
+    _refuse_long(groups=groups, act=act)
     Nb, P, channels = _norm_args(X, gamma, beta)
     if Y is None:
         Y = torch.empty(X.shape, dtype=out_dtype, device=X.device)
@@ -611,6 +619,7 @@ class Layer:
             r = self._calls.mixed_gemm_act(x4, x8, M, x_scale, x_shift, act, out_mode, residual, residual_order, y_scale, Y)
             if r is not NotImplemented:
                 return r
+        _refuse_long(act=act, out_mode=out_mode, residual_order=residual_order)
         _refuse(M >= 0, f"M = {M} is negative")
         Y, code = self._act_args((M, self.N), out_mode, residual, Y)
         flexiq_mixed_gemm_act(self.h, x4, x8, x_shift, M, x_scale, y_scale, act, residual, code, residual_order, out_mode, Y)
@@ -622,6 +631,7 @@ class Layer:
             r = self._calls.mixed_conv_act(x4, x8, Nb, H, W, x_scale, x_shift, act, out_mode, residual, residual_order, y_scale, Y)
             if r is not NotImplemented:
                 return r
+        _refuse_long(Nb=Nb, H=H, W=W, act=act, out_mode=out_mode, residual_order=residual_order)
         _refuse(self.conv is not None and Nb >= 0, "mixed_conv_act needs a convolution layer and a number of images")
         Y, code = self._act_args((Nb, *self._out_pixels(H, W), self.N), out_mode, residual, Y)
         flexiq_mixed_conv_act(self.h, x4, x8, x_shift, Nb, H, W, x_scale, y_scale, act, residual, code, residual_order, out_mode, Y)
@@ -634,6 +644,7 @@ class Layer:
             r = self._calls.mixed_gemm_act_to_slab(x4, x8, M, x_scale, nxt_calls, next_x_scale, act, slab, x_shift, out_order)
             if r is not NotImplemented:
                 return r
+        _refuse_long(act=act, out_order=out_order)
         _refuse(M >= 0, f"M = {M} is negative")
         slab = nxt._act_slab(slab, M)
         flexiq_mixed_gemm_act_to_slab(self.h, x4, x8, x_shift, M, x_scale, nxt.h, next_x_scale, act, out_order, slab)
@@ -645,6 +656,7 @@ class Layer:
             r = self._calls.mixed_conv_act_to_slab(x4, x8, Nb, H, W, x_scale, nxt_calls, next_x_scale, act, slab, x_shift, out_order)
             if r is not NotImplemented:
                 return r
+        _refuse_long(Nb=Nb, H=H, W=W, act=act, out_order=out_order)
         _refuse(self.conv is not None and Nb >= 0, "mixed_conv_act_to_slab needs a convolution layer and a number of images")
         P, Q = self._out_pixels(H, W)
         slab = nxt._act_slab(slab, Nb * P * Q)
@@ -657,6 +669,7 @@ class Layer:
             r = self._calls.group_norm_to_slab(X, groups, gamma, beta, eps, act, x_scale, slab)
             if r is not NotImplemented:
                 return r
+        _refuse_long(groups=groups, act=act)
         Nb, P, channels = _norm_args(X, gamma, beta)
         _refuse(channels == self.K and X.device == self.device, f"X has {channels} channels on {X.device}, the layer takes {self.K} on {self.device}")
         slab = self._act_slab(slab, Nb * P)
