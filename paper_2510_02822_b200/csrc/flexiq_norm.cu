@@ -696,7 +696,7 @@ __global__ void __launch_bounds__(kNormThreads, 2) group_norm_stats_kernel(const
 #pragma unroll
         for (int i = 0; i < S; ++i) {
             mean[i] = shift[i] + off[i];
-            M2[i] = fmaxf(__fmaf_rn(-n * off[i], off[i], M2[i]), 0.f);   // (a NaN: see below)
+            M2[i] = fmaxf(__fmaf_rn(-n * off[i], off[i], M2[i]), 0.f);   // (an infinite sum of squares stays one: the product is not rounded)
             if (off[i] != off[i]) M2[i] = off[i];
         }
     };

@@ -1,4 +1,4 @@
-"""Group normalisation where an image's pieces end with the image, and where a thread has thousands of them.
+"""Group normalisation where an image's pieces end with the image, where a thread has thousands of them, and where squares leave fp32.
 
 Tolerances as in test_gpu_group_norm."""
 import numpy as np
@@ -53,3 +53,34 @@ def test_an_outlier_in_front_of_a_long_image(dev, P, C, groups, t):
     y = fx.group_norm(x, groups, out_dtype=t)
     for i in (0, 100, 295):
         check(y[i:i + 1], *want_and_tolerance(x[i:i + 1], groups, None, None, 1e-5, fx.ACT_NONE))
+
+
+# the three ways of cutting an image, in pieces of one group and of several, wide and scalar
+KINDS = [(40, 1, 768, 1), (3, 1, 3000, 1), (6, 1, 77, 1), (3, 49, 64, 8), (2, 3136, 64, 32), (2, 50, 30, 5), (2, 64, 2056, 8), (1, 30000, 32, 4), (2, 40000, 64, 32), (1, 40000, 12, 3),
+         (1, 984, 435, 1), (1, 66000, 128, 32)]
+
+
+@pytest.mark.parametrize("Nb,P,C,groups", KINDS)
+def test_squares_beyond_fp32(dev, Nb, P, C, groups):
+    """Deviations whose squares leave fp32: the variance is infinite, and what is normalised is zero.  Both where the values of a channel differ and
+    where only the channels of a group do."""
+    beta = torch.linspace(-2, 2, C, device=dev)
+    want = beta.expand(Nb, P, C)
+    g = torch.Generator(device=dev)
+    g.manual_seed(P + C)
+    sign = (torch.randint(0, 2, (Nb, P, C), generator=g, device=dev) * 2 - 1).float()
+    sign[..., 0::C // groups], sign[..., 1::C // groups] = 1.0, -1.0          # (no group of one sign alone)
+    for t in (F32, BF16):
+        for x in (sign, sign[:1, :1].expand(Nb, P, C)):
+            y = fx.group_norm((x * 2.0 ** 66).to(t).contiguous(), groups, None, beta, out_dtype=F32)
+            assert torch.equal(y, want)
+
+
+@pytest.mark.parametrize("C,groups", [(64, 8), (64, 32)])
+def test_squares_beyond_fp32_where_all_means_agree(dev, C, groups):
+    """As many images as let a block take a whole one of 4096 positions, sixteen side by side: the first eight pieces of every thread are 2^66, the
+    next eight its negative, and so on.  Each thread's distances from its first pieces' mean have a sum and squares that cancel but for infinities."""
+    x = torch.where(torch.arange(4096, device=dev) // 128 % 2 == 0, 2.0 ** 66, -2.0 ** 66)[None, :, None].expand(296, 4096, C).contiguous()
+    beta = torch.linspace(-2, 2, C, device=dev)
+    y = fx.group_norm(x, groups, None, beta)
+    assert torch.equal(y, beta.expand(296, 4096, C))
