@@ -524,7 +524,8 @@ int flexiq_choose_tile(int64_t M, int N, int k_blocks, int block_k, int sm_count
 
 /* Test hook, host-only: the form the automatic choice takes for a masked-path convolution on a GPU of sm_count SMs: 0 a plain
  * GEMM (1x1, stride 1, no padding), 1 im2col copies, 2 halo patches with resident weights, 3 halo patches per K block with
- * streamed weights.  The paper has no counterpart. */
+ * streamed weights.  It answers for calls without a residual: a residual takes 22 KB from the operands' ring, so that such a
+ * call may take another form where the patches would just have fitted.  The paper has no counterpart. */
 int flexiq_choose_conv_kind(int Nb, int H, int W, int Cin, int Cout, int R, int S, int stride, int pad, int sm_count, int *kind_out);
 
 /* Test hook: runs the mainloop's bounded wait, with a limit of about a millisecond instead of two seconds, once on

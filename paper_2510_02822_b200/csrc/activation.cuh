@@ -12,7 +12,7 @@
 // put on a.)  With the exponential's 2^-22, F and 2^-23 around the quotient, F is off by at most 2.8e-7 and the result, rounded
 // once, by less than the 2^-21 |v| that is promised; far out on the negative side the error falls with F.
 // A first form, v times a clipped odd polynomial of 13 coefficients, took 10.5 instructions a value and this one takes 6.5 (ViT-B fc1 with GELU
-// over 12,608 rows 41.4 -> 36.4 us).
+// over 12,608 rows 41.4 -> 36.4 us, in the kernel of that time, which could add a residual too; 31.4 now).
 //
 // The bound on a (min drops a NaN, and an infinity becomes a number whose F is 0) keeps one value of a pair from
 // spoiling the other and gives infinities their limits; max.NaN passes a NaN on.

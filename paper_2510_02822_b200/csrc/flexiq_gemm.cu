@@ -60,7 +60,8 @@ constexpr int kOutScatter = 6;
 // and 180 loaded in the plain CTA pair, 108 and 244 in the single CTA, none in either now), and the epilogue is as long as the mainloop
 // at short K.  Packed path, 768 -> 3072 at 12,608 rows 60.7 -> 57.1 us, 384 -> 1536 at 1576 8.9 -> 7.8.
 // The kinds from kKindActI8 on apply an activation, those from kKindResI8 on add a residual too: more instructions and registers, and so kernels
-// of their own (768 -> 3072 at 12,608 rows, GELU, fp16: 41.6 us where one kernel may add a residual too, 32.7 in one that cannot).
+// of their own (768 -> 3072 at 12,608 rows, GELU, back to back, in a kernel that cannot add a residual and in one that can: fp16 31.4 and 40.0 us, int8 33.2
+// and 42.5, fp32 40.0 and 46.7; int8 without an activation 20.3 in the plain kernel, 23.4 in the one that can apply one).
 enum OutKind { kKindI8, kKindNext, kKindScatter, kKindHalf, kKindWord, kKindActI8, kKindActNext, kKindActScatter, kKindActHalf, kKindActWord,
                kKindResI8, kKindResHalf, kKindResWord };
 static OutKind out_kind(int out_mode, bool staged)
@@ -481,7 +482,7 @@ __device__ __forceinline__ void epilogue_role(const GemmParams &p, const Epilogu
     // A residual comes through shared memory, 64 bytes of the warp's 32 rows at a time (16-bit: 32 columns, fp32: 16), by asynchronous
     // copies of whole 64-byte pieces: the next piece, of the next tile where this one ends, is under way while one is worked on.  With each
     // lane loading from its own row (32 bytes of 32 lines an instruction) the requests were the limit, whatever their width: 768 -> 3072 at
-    // 12,608 rows, fp16, 57.2 us (47 without allocation in L1), 43.7 so.  The 16-byte chunks of a row lie permuted, so that neither side
+    // 12,608 rows, fp16, 57.2 us (47 without allocation in L1), 43.7 so, and 39.9 since the kernels with a residual are their own.  The 16-byte chunks of a row lie permuted, so that neither side
     // meets a bank twice.  The ring gives up 22 KB for it: five stages of a 256-column pair's six, which costs nothing at 768 channels and up
     // to 5 % at 3072 (four stages 15 %, hence no more than 64 bytes of a row at a time).
     const int res_log = p.res_dtype == FLEXIQ_DTYPE_F32 ? 2 : 1;   // bytes of a value
@@ -638,7 +639,7 @@ __device__ __forceinline__ void epilogue_role(const GemmParams &p, const Epilogu
                     finish16_act<RES>(p, r, x.fac + 16 * u, x.fac + 64 + 16 * u, res, v);
                     if (kScatterOut) {
                         // a chunk is a box of 16 columns wherever it goes; two of them are under way (768 -> 3072 at 12,608 rows into slab order of 16-channel
-                        // groups: 29.7 us, by 16-byte stores from the lanes 34.6; with GELU 40.1 and 42.8)
+                        // groups, back to back: 27.7 us, by 16-byte stores from the lanes 32.4; with GELU 37 both)
                         const int ent_u = u == 0 ? ents[0] : u == 1 ? ents[1] : u == 2 ? ents[2] : ents[3];
                         uint32_t w[4];
                         quantize16_next(p, ent_u, v, w);
