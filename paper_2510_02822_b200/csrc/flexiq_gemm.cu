@@ -49,6 +49,13 @@ constexpr int kResPerWarp = 2048;                     // 32 rows x 64 bytes
 constexpr int kStageRegionRes = 174080;
 constexpr int kSmemBytesRes = kStageRegionRes + kNumWorkWarps * (kFactorsPerWarp + kStoreStagePerWarp + kResPerWarp) + 256;
 static_assert(kSmemBytesRes <= 232448, "shared memory of a block");
+// Not on the packed path: its ring must have three stages.  The producer only counts the stages of the blocks that the expanders fill, and is up to
+// kRawStages of them ahead; it waits for a stage again at the next 8-bit block, by a parity, which says what it should only when the stage's fill
+// before the last has been consumed.  With three stages that follows from the raw tile the producer has been given back; with two it does not,
+// and a copy may land in a stage that is still being read.  The eight epilogue warps there leave room for a residual behind the whole ring.
+constexpr int kPackedEpiWarps = 8;
+static_assert(kStageRegion - kRawStages * (BM + 256) * 64 >= 3 * (BM + 256) * 128, "three stages of the widest tile on the packed path");
+static_assert(kStageRegion + kPackedEpiWarps * (kFactorsPerWarp + kStoreStagePerWarp + kResPerWarp) + 256 <= kSmemBytesRes, "the packed path's layout with a residual");
 
 // Internal epilogue mode of the fused layer boundary: the int8 result goes straight into the
 // next layer's masked slab (its channel order, its low groups lowered).
@@ -885,9 +892,12 @@ mixed_gemm_kernel(const __grid_constant__ CUtensorMap mapA_lo, const __grid_cons
         return;
     }
     uint8_t *stage_base = smem;
-    uint8_t *factors = smem + (OUT >= kKindResI8 ? kStageRegionRes : kStageRegion);
-    uint8_t *store_stage = factors + kNumWorkWarps * kFactorsPerWarp;  // 1024-byte aligned: the bulk stores' swizzle needs it
-    uint64_t *full_bar = reinterpret_cast<uint64_t *>(store_stage + kNumWorkWarps * kStoreStagePerWarp);
+    constexpr bool kRes = OUT >= kKindResI8;
+    constexpr int kEpiWarps = PK ? kPackedEpiWarps : 16;
+    constexpr int kLaidOut = PK && kRes ? kEpiWarps : kNumWorkWarps;    // warps with factors and staging of their own
+    uint8_t *factors = smem + (kRes && !PK ? kStageRegionRes : kStageRegion);
+    uint8_t *store_stage = factors + kLaidOut * kFactorsPerWarp;  // 1024-byte aligned: the bulk stores' swizzle needs it
+    uint64_t *full_bar = reinterpret_cast<uint64_t *>(store_stage + kLaidOut * kStoreStagePerWarp);
     uint64_t *empty_bar = full_bar + kMaxStages;
     uint64_t *tmem_full = empty_bar + kMaxStages;
     uint64_t *tmem_empty = tmem_full + 4;
@@ -895,7 +905,6 @@ mixed_gemm_kernel(const __grid_constant__ CUtensorMap mapA_lo, const __grid_cons
     uint64_t *raw_empty = raw_full + kRawStages;
     uint64_t *turn_bar = raw_empty + kRawStages;     // hand-over between the two MMA warps: one phase per tile
     uint32_t *tmem_ptr_s = reinterpret_cast<uint32_t *>(turn_bar + 1);
-    constexpr int kEpiWarps = PK ? 8 : 16;
     constexpr int kExpWarps = PK ? 8 : 0;
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_ptr_s + 1);
 
@@ -1497,11 +1506,11 @@ mixed_gemm_kernel(const __grid_constant__ CUtensorMap mapA_lo, const __grid_cons
             x.tmem_full = tmem_full; x.tmem_empty = tmem_empty; x.abort_flag = abort_flag;
             x.fac = reinterpret_cast<float *>(factors + e * kFactorsPerWarp);  // alpha[64] | beta[64]
             x.store_stage = ptx::smem_u32(store_stage + e * kStoreStagePerWarp);
-            x.res_stage = ptx::smem_u32(store_stage + kNumWorkWarps * kStoreStagePerWarp + 256 + e * kResPerWarp);
+            x.res_stage = ptx::smem_u32(store_stage + kLaidOut * kStoreStagePerWarp + 256 + e * kResPerWarp);
             x.map_y = &mapY; x.map_y16 = &mapY16;
             x.first_tile = first_tile; x.tile_step = tile_step; x.num_tiles = num_tiles;
             x.parts = kEpiWarps / 4; x.arrivals_on = 1;
-            constexpr bool kAct = OUT >= kKindActI8, kRes = OUT >= kKindResI8;
+            constexpr bool kAct = OUT >= kKindActI8;
             if constexpr (OUT == kKindI8 || OUT == kKindActI8 || OUT == kKindResI8) epilogue_role<CG, FLEXIQ_OUT_REQUANT_I8, SPLIT, KIND, kAct, kRes>(p, x, warp & 3, e >> 2, lane);
             else if constexpr (OUT == kKindNext || OUT == kKindActNext) epilogue_role<CG, kOutNextSlab, SPLIT, KIND, kAct>(p, x, warp & 3, e >> 2, lane);
             else if constexpr (OUT == kKindScatter || OUT == kKindActScatter) epilogue_role<CG, kOutScatter, SPLIT, KIND, kAct>(p, x, warp & 3, e >> 2, lane);
@@ -2022,7 +2031,7 @@ static int run_mixed(Layer *L, const uint8_t *X4, const int8_t *X8, const uint8_
     } else if ((rc = check_slab(L, X4, "X4_dev"))) return rc;
     const int sms = device_sm_count(L->device);
 
-    const int region = ops && ops->res ? kStageRegionRes : kStageRegion;
+    const int region = ops && ops->res && !packed ? kStageRegionRes : kStageRegion;
     GemmParams p{};
     p.M = M; p.N = L->N; p.C = L->C; p.C_lo = packed ? C_lo : 0; p.C_hi = packed ? C_hi : L->C;
     p.T = L->R * L->S; p.S = L->S;
