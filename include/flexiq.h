@@ -341,7 +341,7 @@ int flexiq_mixed_conv_act_to_slab(flexiq_layer_t layer, const uint8_t *X4_dev, c
 int flexiq_group_norm(const void *X_dev, int x_dtype, int64_t Nb, int64_t P, int C, int groups,
                       const float *gamma_dev, const float *beta_dev, float eps, int act, int y_dtype, void *Y_dev,
                       void *scratch_dev, void *stream);
-/* Bytes of scratch flexiq_group_norm and flexiq_group_norm_to_slab need for a shape (host-only). */
+/* Bytes of scratch flexiq_group_norm and flexiq_group_norm_to_slab need for a shape on the current device (host-only). */
 int flexiq_group_norm_scratch(int x_dtype, int64_t Nb, int64_t P, int C, int groups, int64_t *bytes_out);
 
 /* The same, into the activation slab of `layer` (C = its input channels) in place of a floating-point tensor:
